@@ -92,6 +92,30 @@ typedef struct {
   int64_t stride_page;
 } dustin_kv;
 
+/* A K or V cache of one layer held in 4 bits.  A row of head_dim channels is head_dim / 32 blocks of 32 channels in
+ * the OCP Microscaling format MXFP4: an element is an E2M1 code (bit 3 the sign; 0, 0.5, 1, 1.5, 2, 3, 4, 6), two to a
+ * byte, the even channel in the low half, and a block has one scale byte e, for 2^(e - 127).
+ *   contiguous: channel c of (b, n, g) is half (c % 2) of data[b * stride_b + n * stride_n + g * stride_h + c / 2], its
+ *       scale scales[b * scale_stride_b + n * scale_stride_n + g * scale_stride_h + c / 32]
+ *   paged: as dustin_kv, with stride_page and scale_stride_page in place of the sequence strides
+ * Strides are in BYTES.  data and its strides are multiples of 16; scales and its strides of head_dim / 32.  K and V
+ * of one call share the page table and page size.  Zeroed memory is a valid cache (of zeros), and rows that
+ * dustin_kv4_append wrote are always finite; other scale bytes than 0 and 2 ... 252 are the caller's business. */
+typedef struct {
+  const void* data;
+  const void* scales;
+  int32_t num_kv_heads;
+  int32_t head_dim;            /* 64 or 128 (attention: 128)                           */
+  int64_t stride_b, stride_n, stride_h;
+  int64_t scale_stride_b, scale_stride_n, scale_stride_h;
+  int64_t capacity;            /* positions addressable per sequence (contiguous mode) */
+  const int32_t* page_table;   /* NULL = contiguous; else device int32 [B, max_pages]  */
+  int32_t page_size;           /* paged: a power of two                                */
+  int32_t max_pages;
+  int32_t num_pages;
+  int64_t stride_page, scale_stride_page;
+} dustin_kv4;
+
 /* Per-sequence sizes.  A NULL device array means "the scalar for every sequence". */
 typedef struct {
   int32_t batch;               /* B                                                    */
@@ -484,6 +508,81 @@ dustin_status dustin_kv_append(const void* k_new, int64_t k_sb, int64_t k_st, in
  * --------------------------------------------------------------------------------- */
 dustin_status dustin_kv_commit(int32_t* seq_lens, const int32_t* accepted, const int32_t* n_query,
                                int32_t batch, int32_t nq_max, void* stream);
+
+/* ---------------------------------------------------------------------------------
+ * dustin_kv4_append -- dustin_kv_append into 4-bit caches: the rows of the verification window, or of a prompt, are
+ * rounded into the format.  A block's scale is 2^(E - 2), with 2^E <= its largest magnitude < 2^(E + 1) (E - 2 not
+ * below -125); each channel over the scale is the nearest element, of two as near the one with an even code, and 6
+ * beyond 6.  An infinity counts as the largest finite bf16 of its sign, a NaN as zero.
+ *   k_new, v_new  bf16 [B, nq_max, Hkv, d] (d 64 or 128), strides in elements, as dustin_kv_append
+ *   k, v          the caches; must address max_len + nq_max positions per sequence
+ *   bt            seq_lens (N_b), n_query (T_b, NULL = nq_max), max_len, nq_max
+ * --------------------------------------------------------------------------------- */
+dustin_status dustin_kv4_append(const void* k_new, int64_t k_sb, int64_t k_st, int64_t k_sh, const void* v_new,
+                                int64_t v_sb, int64_t v_st, int64_t v_sh, const dustin_kv4* k, const dustin_kv4* v,
+                                const dustin_batch* bt, void* stream);
+
+/* ---------------------------------------------------------------------------------
+ * dustin_kv4_read -- the values of positions [N_b, N_b + T_b) of 4-bit caches, as bf16 (exact):
+ *   k_out[b, t, h, :] = K[b, N_b + t, h, :], v_out alike, for t < T_b; other rows of the outputs are not written.
+ * With N_b = 0 and T_b the context it reads whole caches, for the entry points that take a bf16 cache (the scores).
+ * Arguments as dustin_kv4_append's, with outputs in place of k_new and v_new.
+ * --------------------------------------------------------------------------------- */
+dustin_status dustin_kv4_read(void* k_out, int64_t k_sb, int64_t k_st, int64_t k_sh, void* v_out, int64_t v_sb,
+                              int64_t v_st, int64_t v_sh, const dustin_kv4* k, const dustin_kv4* v,
+                              const dustin_batch* bt, void* stream);
+
+/* ---------------------------------------------------------------------------------
+ * dustin_sparse_verify_attn_kv4, dustin_dense_verify_attn_kv4 -- dustin_sparse_verify_attn and dense_verify_attn over
+ * 4-bit caches of 128 channels: the same sums, with K and V the values that the caches stand for.  Arguments, limits
+ * and rounding are theirs, but for
+ *   - the caches' rows may lie anywhere a 64-bit offset reaches, pages need not be packed;
+ *   - workspace: dustin_attn_kv4_workspace(...) bytes, 256-byte aligned, of any content.  Calls that share a
+ *     workspace must not overlap.
+ * max_tokens of the workspace is k_max (sparse) or max_len (dense).  batch * num_kv_heads <= 65536.
+ * --------------------------------------------------------------------------------- */
+size_t dustin_attn_kv4_workspace(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t nq_max,
+                                 int32_t max_tokens);
+dustin_status dustin_sparse_verify_attn_kv4(const void* q, int64_t q_sb, int64_t q_st, int64_t q_sh,
+                                            int32_t num_q_heads, const dustin_kv4* k, const dustin_kv4* v,
+                                            const dustin_batch* bt, const int32_t* idx, int64_t idx_sb, int64_t idx_sg,
+                                            const int32_t* count, int32_t groups, float scale, void* out, int64_t o_sb,
+                                            int64_t o_st, int64_t o_sh, void* workspace, size_t workspace_bytes,
+                                            void* stream);
+dustin_status dustin_dense_verify_attn_kv4(const void* q, int64_t q_sb, int64_t q_st, int64_t q_sh,
+                                           int32_t num_q_heads, const dustin_kv4* k, const dustin_kv4* v,
+                                           const dustin_batch* bt, float scale, void* out, int64_t o_sb, int64_t o_st,
+                                           int64_t o_sh, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------
+ * dustin_kv_evict, dustin_kv4_evict -- eviction: a layer's cache cut to its kept rows, in their order.  The kept
+ * positions are a selection as dustin_topk writes it, made by accumulated attention weight: dustin_score with init =
+ * the weights so far adds a step's attention to them, and dustin_topk with s_target = the weights and m = 0 keeps
+ * n_sink sinks, n_window recent positions and the best of the others.
+ *   K_out[b, i, g, :] = K[b, idx[b, gi, i], g, :], V alike, for i < count[b, gi]   (gi = g if groups > 1 else 0)
+ *   w_out[b, go, i]   = w[b, go, idx[b, go, i]]
+ *   new_lens[b]       = count[b, 0]
+ * with count clamped to [0, k_max]; rows from count on are not written.  After it the cache holds new_lens[b]
+ * positions, whose order is that of the old ones.
+ *   k, v, k_out, v_out  caches of 64 or 128 channels.  k_out and v_out are other caches (other pages), or the same:
+ *       equal data, strides and page tables mark the call as in place.  Caches that overlap in another way are not
+ *       supported, nor is one of K and V in place alone (DUSTIN_ERR_INVALID_ARG).  k_out and v_out address at least
+ *       k_max positions.
+ *   idx, count  int32 [B, groups, >= k_max] (strides idx_sb, idx_sg) and [B * groups]; ascending positions (in place,
+ *       others give rows of unspecified content); groups 1 or the KV head count
+ *   w, w_out    fp32 [B, groups, >= w_len], [B, groups, >= k_max] (strides in elements) or both NULL; w_out may be w
+ *   new_lens    int32 [B] or NULL; may be the batch's seq_lens, which this call does not read
+ * A step's layers share idx: pass w and new_lens with one of them.
+ * --------------------------------------------------------------------------------- */
+dustin_status dustin_kv_evict(const dustin_kv* k, const dustin_kv* v, const dustin_kv* k_out, const dustin_kv* v_out,
+                              int32_t batch, const int32_t* idx, int64_t idx_sb, int64_t idx_sg, const int32_t* count,
+                              int32_t groups, int32_t k_max, const float* w, int64_t w_sb, int64_t w_sg, int32_t w_len,
+                              float* w_out, int64_t wo_sb, int64_t wo_sg, int32_t* new_lens, void* stream);
+dustin_status dustin_kv4_evict(const dustin_kv4* k, const dustin_kv4* v, const dustin_kv4* k_out,
+                               const dustin_kv4* v_out, int32_t batch, const int32_t* idx, int64_t idx_sb,
+                               int64_t idx_sg, const int32_t* count, int32_t groups, int32_t k_max, const float* w,
+                               int64_t w_sb, int64_t w_sg, int32_t w_len, float* w_out, int64_t wo_sb, int64_t wo_sg,
+                               int32_t* new_lens, void* stream);
 
 /* ---------------------------------------------------------------------------------
  * dustin_read_probe -- a plain streaming read of a device buffer, for measurement only (no

@@ -16,7 +16,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
-from typing import Optional, Sequence
+from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch
 
@@ -30,7 +30,10 @@ EXPORTED = ("dustin_status_string", "dustin_version", "dustin_score_workspace", 
             "dustin_sparse_verify_attn", "dense_verify_attn", "dustin_kv_append", "dustin_kv_commit",
             "dustin_score_layers", "dustin_page_meta", "dustin_page_score_workspace",
             "dustin_page_score", "dustin_arr", "dustin_score_per_layer",
-            "dustin_sparse_verify_attn_noalloc", "dustin_score_calls", "dustin_read_probe")
+            "dustin_sparse_verify_attn_noalloc", "dustin_score_calls", "dustin_read_probe",
+            "dustin_kv4_append", "dustin_kv4_read", "dustin_attn_kv4_workspace",
+            "dustin_sparse_verify_attn_kv4", "dustin_dense_verify_attn_kv4", "dustin_kv_evict",
+            "dustin_kv4_evict")
 
 
 class DustinError(RuntimeError):
@@ -46,6 +49,16 @@ class DustinKV(ctypes.Structure):
                 ("capacity", ctypes.c_int64), ("page_table", ctypes.c_void_p),
                 ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32),
                 ("num_pages", ctypes.c_int32), ("stride_page", ctypes.c_int64)]
+
+
+class DustinKV4(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("num_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("stride_b", ctypes.c_int64), ("stride_n", ctypes.c_int64),
+                ("stride_h", ctypes.c_int64), ("scale_stride_b", ctypes.c_int64),
+                ("scale_stride_n", ctypes.c_int64), ("scale_stride_h", ctypes.c_int64),
+                ("capacity", ctypes.c_int64), ("page_table", ctypes.c_void_p), ("page_size", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("stride_page", ctypes.c_int64),
+                ("scale_stride_page", ctypes.c_int64)]
 
 
 class DustinBatch(ctypes.Structure):
@@ -135,6 +148,23 @@ def lib():
         L.dustin_kv_commit.argtypes = [_vp, _vp, _vp, _i32, _i32, _vp]
         L.dustin_read_probe.restype = ctypes.c_int
         L.dustin_read_probe.argtypes = [_vp, _sz, _vp, _i32, _vp]
+        P_KV4 = ctypes.POINTER(DustinKV4)
+        L.dustin_kv4_append.restype = ctypes.c_int
+        L.dustin_kv4_append.argtypes = [_vp, _i64, _i64, _i64, _vp, _i64, _i64, _i64, P_KV4, P_KV4, P_BT, _vp]
+        L.dustin_kv4_read.restype = ctypes.c_int
+        L.dustin_kv4_read.argtypes = L.dustin_kv4_append.argtypes
+        L.dustin_attn_kv4_workspace.restype = _sz
+        L.dustin_attn_kv4_workspace.argtypes = [_i32, _i32, _i32, _i32, _i32]
+        L.dustin_sparse_verify_attn_kv4.restype = ctypes.c_int
+        L.dustin_sparse_verify_attn_kv4.argtypes = [_vp, _i64, _i64, _i64, _i32, P_KV4, P_KV4, P_BT, _vp, _i64, _i64,
+                                                    _vp, _i32, ctypes.c_float, _vp, _i64, _i64, _i64, _vp, _sz, _vp]
+        L.dustin_dense_verify_attn_kv4.restype = ctypes.c_int
+        L.dustin_dense_verify_attn_kv4.argtypes = [_vp, _i64, _i64, _i64, _i32, P_KV4, P_KV4, P_BT, ctypes.c_float,
+                                                   _vp, _i64, _i64, _i64, _vp, _sz, _vp]
+        for f, P in ((L.dustin_kv_evict, P_KV), (L.dustin_kv4_evict, P_KV4)):
+            f.restype = ctypes.c_int
+            f.argtypes = [P, P, P, P, _i32, _vp, _i64, _i64, _vp, _i32, _i32, _vp, _i64, _i64, _i32, _vp, _i64, _i64,
+                          _vp, _vp]
         _lib = L
     return _lib
 
@@ -817,3 +847,238 @@ def plan_kv_commit(seq_lens: torch.Tensor, accepted: torch.Tensor, *, n_query=No
 def kv_commit(seq_lens, accepted, **kw):
     """N_b += accepted_b (clamped to [0, T_b]); returns seq_lens."""
     return plan_kv_commit(seq_lens, accepted, **kw)()
+
+
+# ----------------------------------------------------------------------------- 4-bit caches
+
+KV4_BLOCK = 32  # channels that share a scale
+
+
+class KV4(NamedTuple):
+    """A K or V cache held in 4 bits (MXFP4; dustin_kv4): data uint8 [B, N_cap, Hkv, d / 2] (two channels a byte) and
+    scales uint8 [B, N_cap, Hkv, d / 32], or [num_pages, page_size, Hkv, ...] with a page table."""
+    data: torch.Tensor
+    scales: torch.Tensor
+
+
+def kv4_empty(B: int, n: int, num_kv_heads: int, head_dim: int, device) -> Tuple[KV4, KV4]:
+    """Zeroed K and V caches of B sequences of n positions (or of B pages of n positions), with a head's K and V rows
+    side by side: the attention reads both, and together they are the 128 bytes that memory moves at once."""
+    data = torch.zeros((B, n, num_kv_heads, 2, head_dim // 2), dtype=torch.uint8, device=device)
+    scales = torch.zeros((B, n, num_kv_heads, 2, head_dim // KV4_BLOCK), dtype=torch.uint8, device=device)
+    return KV4(data[..., 0, :], scales[..., 0, :]), KV4(data[..., 1, :], scales[..., 1, :])
+
+
+def kv4_view(cache: KV4, page_table: Optional[torch.Tensor] = None) -> DustinKV4:
+    """dustin_kv4 of a 4-bit cache (contiguous, or paged with an int32 page table [B, max_pages])."""
+    data, scales = cache
+    for t in (data, scales):
+        if t.dtype != torch.uint8 or t.dim() != 4 or t.stride(3) != 1:
+            raise ValueError("a 4-bit cache is uint8 data [B|pages, N|page_size, Hkv, d / 2] and scales [..., d / 32], "
+                             "with contiguous rows")
+    if data.shape[:3] != scales.shape[:3] or data.shape[3] * 2 != scales.shape[3] * KV4_BLOCK:
+        raise ValueError(f"scales {tuple(scales.shape)} do not belong to data {tuple(data.shape)}")
+    kv = DustinKV4()
+    kv.data, kv.scales = data.data_ptr(), scales.data_ptr()
+    kv.num_kv_heads, kv.head_dim = data.shape[2], 2 * data.shape[3]
+    kv.stride_n, kv.stride_h = data.stride(1), data.stride(2)
+    kv.scale_stride_n, kv.scale_stride_h = scales.stride(1), scales.stride(2)
+    if page_table is None:
+        kv.stride_b, kv.scale_stride_b = data.stride(0), scales.stride(0)
+        kv.capacity = data.shape[1]
+    else:
+        if page_table.dtype != torch.int32 or page_table.dim() != 2:
+            raise ValueError("page_table must be int32 [B, max_pages]")
+        page_table = page_table.contiguous()
+        kv.page_table = page_table.data_ptr()
+        kv.page_size, kv.max_pages, kv.num_pages = data.shape[1], page_table.shape[1], data.shape[0]
+        kv.stride_page, kv.scale_stride_page = data.stride(0), scales.stride(0)
+        kv._keep = page_table
+    return kv
+
+
+def _kv4_pair(k: KV4, v: KV4, page_table) -> Tuple[DustinKV4, DustinKV4]:
+    """The views of K and V, which share the page table (one copy of it if it is not contiguous)."""
+    _on_gpu(*k, *v, page_table)
+    if page_table is not None:
+        page_table = page_table.contiguous()
+    return kv4_view(k, page_table), kv4_view(v, page_table)
+
+
+def _kv4_rows(fn, what, k_rows, v_rows, k, v, seq_lens, n_query, page_table, max_len, stream, result) -> Call:
+    _on_gpu(k_rows, v_rows)
+    kv, vv = _kv4_pair(k, v, page_table)
+    for t in (k_rows, v_rows):
+        if t.dtype != torch.bfloat16 or t.dim() != 4 or t.stride(3) != 1:
+            raise ValueError("rows must be bf16 [B, T, Hkv, d] with contiguous d")
+        if t.shape != k_rows.shape or t.shape[2] != kv.num_kv_heads or t.shape[3] != kv.head_dim:
+            raise ValueError(f"rows {tuple(t.shape)} do not fit caches of {kv.num_kv_heads} heads of {kv.head_dim}")
+    B, nq_max = k_rows.shape[0], k_rows.shape[1]
+    if page_table is None and k.data.shape[0] < B:
+        raise ValueError("the cache holds fewer sequences than there are rows")
+    dev = k_rows.device
+    max_len = _capacity(kv) - nq_max if max_len is None else int(max_len)
+    seq, nqa = _i32_dev(seq_lens, dev), _i32_dev(n_query, dev)
+    bt = _batch(B, max_len, nq_max, 0, seq, nqa)
+    args = (_ptr(k_rows), k_rows.stride(0), k_rows.stride(1), k_rows.stride(2), _ptr(v_rows), v_rows.stride(0),
+            v_rows.stride(1), v_rows.stride(2), ctypes.byref(kv), ctypes.byref(vv), ctypes.byref(bt), _stream(stream))
+    return Call(fn, args, what, (k_rows, v_rows, k, v, kv, vv, bt), result)
+
+
+def plan_kv4_append(k_new: torch.Tensor, v_new: torch.Tensor, k: KV4, v: KV4, seq_lens, *, n_query=None,
+                    page_table: Optional[torch.Tensor] = None, max_len: Optional[int] = None, stream=None) -> Call:
+    """Prepared dustin_kv4_append: k_new / v_new bf16 [B, T_max, Hkv, d] go, rounded into 4 bits, to positions
+    [N_b, N_b + T_b) of the caches."""
+    return _kv4_rows(lib().dustin_kv4_append, "dustin_kv4_append", k_new, v_new, k, v, seq_lens, n_query, page_table,
+                     max_len, stream, None)
+
+
+def kv4_append(k_new, v_new, k, v, seq_lens, **kw):
+    """Writes the window's (or a prompt's) K and V into the 4-bit caches at [N_b, N_b + T_b)."""
+    return plan_kv4_append(k_new, v_new, k, v, seq_lens, **kw)()
+
+
+def plan_kv4_read(k: KV4, v: KV4, seq_lens, *, n_query=None, nq_max: Optional[int] = None,
+                  page_table: Optional[torch.Tensor] = None, max_len: Optional[int] = None,
+                  k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None, stream=None) -> Call:
+    """Prepared dustin_kv4_read: the values of positions [N_b, N_b + T_b) as bf16 [B, T_max, Hkv, d] (rows from T_b on
+    are not written; outputs made here hold zeros there).  T_max is nq_max, or that of the outputs given."""
+    if (k_out is None) != (v_out is None):
+        raise ValueError("give both outputs or neither")
+    if k_out is None:
+        if nq_max is None:
+            raise ValueError("kv4_read needs nq_max or outputs")
+        B = seq_lens.shape[0] if isinstance(seq_lens, torch.Tensor) else len(seq_lens)
+        shape = (B, int(nq_max), k.data.shape[2], 2 * k.data.shape[3])
+        k_out = torch.zeros(shape, dtype=torch.bfloat16, device=k.data.device)
+        v_out = torch.zeros_like(k_out)
+    return _kv4_rows(lib().dustin_kv4_read, "dustin_kv4_read", k_out, v_out, k, v, seq_lens, n_query, page_table,
+                     max_len, stream, (k_out, v_out))
+
+
+def kv4_read(k, v, seq_lens, **kw):
+    """The values of cache rows [N_b, N_b + T_b); returns (k_out, v_out)."""
+    return plan_kv4_read(k, v, seq_lens, **kw)()
+
+
+def _plan_attn_kv4(q, k, v, idx, count, seq_lens, n_query, page_table, scale, out, max_len, stream) -> Call:
+    _on_gpu(q, out, idx, count)
+    kv, vv = _kv4_pair(k, v, page_table)
+    if q.dtype != torch.bfloat16 or q.dim() != 4 or q.stride(3) != 1:
+        raise ValueError("q must be bf16 [B, T, Hq, 128] with contiguous rows")
+    B, nq_max, Hq, d = q.shape
+    if d != kv.head_dim or (page_table is None and k.data.shape[0] < B):
+        raise ValueError(f"q {tuple(q.shape)} does not fit the caches")
+    if out is None:
+        out = torch.empty_like(q)
+    if out.dtype != torch.bfloat16 or out.shape != q.shape or out.stride(3) != 1:
+        raise ValueError("out must be bf16 of q's shape with contiguous rows")
+    dev = q.device
+    max_len = _capacity(kv) - nq_max if max_len is None else int(max_len)
+    seq, nqa = _i32_dev(seq_lens, dev), _i32_dev(n_query, dev)
+    scale = 1.0 / math.sqrt(d) if scale is None else scale
+    k_max = 0 if idx is None else idx.shape[2]
+    bt = _batch(B, max_len, nq_max, k_max, seq, nqa)
+    nbytes = lib().dustin_attn_kv4_workspace(B, Hq, kv.num_kv_heads, nq_max, max_len if idx is None else k_max)
+    ws = workspace(nbytes, dev, "attn_kv4", stream)
+    head = (_ptr(q), q.stride(0), q.stride(1), q.stride(2), Hq, ctypes.byref(kv), ctypes.byref(vv), ctypes.byref(bt))
+    tail = (float(scale), _ptr(out), out.stride(0), out.stride(1), out.stride(2), _ptr(ws), nbytes, _stream(stream))
+    keep = (q, k, v, idx, count, kv, vv, bt, ws)
+    if idx is None:
+        return Call(lib().dustin_dense_verify_attn_kv4, head + tail, "dustin_dense_verify_attn_kv4", keep, out)
+    sel = (_ptr(idx), idx.stride(0), idx.stride(1), _ptr(count), idx.shape[1])
+    return Call(lib().dustin_sparse_verify_attn_kv4, head + sel + tail, "dustin_sparse_verify_attn_kv4", keep, out)
+
+
+def _selection(idx, count, B):
+    """(idx, count) as dustin_topk writes them: int32 [B, G, k_max] contiguous in k, int32 [B, G]."""
+    if idx.dtype != torch.int32 or idx.dim() != 3 or idx.shape[0] < B or idx.stride(2) != 1:
+        raise ValueError("idx must be int32 [B, G, k_max] with contiguous entries")
+    if count.dtype != torch.int32 or tuple(count.shape) != tuple(idx.shape[:2]):
+        raise ValueError("count must be int32 [B, G] for idx [B, G, k_max]")
+    return count.contiguous()
+
+
+def plan_sparse_verify_attn_kv4(q: torch.Tensor, k: KV4, v: KV4, idx: torch.Tensor, count: torch.Tensor, seq_lens, *,
+                                n_query=None, page_table: Optional[torch.Tensor] = None,
+                                scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                                max_len: Optional[int] = None, stream=None) -> Call:
+    """Prepared verification attention over idx[b, g, :count] of 4-bit caches plus the causal verification window.
+    q / out bf16 [B, T_max, Hq, 128]; idx int32 [B, G, k_max]; count int32 [B, G]."""
+    count = _selection(idx, count, q.shape[0])
+    return _plan_attn_kv4(q, k, v, idx, count, seq_lens, n_query, page_table, scale, out, max_len, stream)
+
+
+def sparse_verify_attn_kv4(q, k, v, idx, count, seq_lens, **kw):
+    """Verification attention over a selection of 4-bit caches; returns out (rows t >= T_b untouched)."""
+    return plan_sparse_verify_attn_kv4(q, k, v, idx, count, seq_lens, **kw)()
+
+
+def plan_dense_verify_attn_kv4(q: torch.Tensor, k: KV4, v: KV4, seq_lens, *, n_query=None,
+                               page_table: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                               out: Optional[torch.Tensor] = None, max_len: Optional[int] = None,
+                               stream=None) -> Call:
+    """Prepared full-cache verification attention over 4-bit caches."""
+    return _plan_attn_kv4(q, k, v, None, None, seq_lens, n_query, page_table, scale, out, max_len, stream)
+
+
+def dense_verify_attn_kv4(q, k, v, seq_lens, **kw):
+    """Full-cache verification attention over 4-bit caches; returns out (rows t >= T_b untouched)."""
+    return plan_dense_verify_attn_kv4(q, k, v, seq_lens, **kw)()
+
+
+# ----------------------------------------------------------------------------- eviction
+
+def plan_kv_evict(k, v, idx: torch.Tensor, count: torch.Tensor, *, k_out=None, v_out=None,
+                  page_table: Optional[torch.Tensor] = None, out_page_table: Optional[torch.Tensor] = None,
+                  weights: Optional[torch.Tensor] = None, weights_out: Optional[torch.Tensor] = None,
+                  new_lens: Optional[torch.Tensor] = None, stream=None) -> Call:
+    """Prepared dustin_kv_evict (bf16 caches) or dustin_kv4_evict (KV4): a layer's rows idx[b, g, :count] to the front
+    of k_out / v_out (with out_page_table), or of the caches themselves where no outputs are given.  weights fp32
+    [B, G, N] go the same way into weights_out (None: in place), new_lens int32 [B] becomes the counts."""
+    four = isinstance(k, KV4)
+    if (k_out is None) != (v_out is None) or any(isinstance(x, KV4) != four for x in (v, k_out, v_out) if x is not None):
+        raise ValueError("k, v, k_out and v_out are bf16 caches or KV4 caches, both outputs or neither given")
+    if k_out is None:
+        if out_page_table is not None:
+            raise ValueError("in place, the pages stay: out_page_table goes with outputs")
+        k_out, v_out, out_page_table = k, v, page_table
+    B, G, k_max = idx.shape
+    _on_gpu(idx, count, weights, weights_out, new_lens)
+    count = _selection(idx, count, B)
+    tables = [None if t is None else t.contiguous() for t in (page_table, out_page_table)]
+    if page_table is out_page_table:
+        tables[1] = tables[0]
+    if four:
+        views = [x for pair, t in zip(((k, v), (k_out, v_out)), tables) for x in _kv4_pair(*pair, t)]
+    else:
+        _on_gpu(k, v, k_out, v_out, page_table, out_page_table)
+        views = [kv_view(x, t) for pair, t in zip(((k, v), (k_out, v_out)), tables) for x in pair]
+    for x, t in zip((k, k_out), tables):
+        n = t.shape[0] if t is not None else (x.data if four else x).shape[0]
+        if n < B:
+            raise ValueError("the caches hold fewer sequences than idx")
+    if weights is None and weights_out is not None:
+        raise ValueError("weights_out goes with weights")
+    ws = (0, 0, 0, 0, 0)
+    if weights is not None:
+        weights_out = weights if weights_out is None else weights_out
+        n = weights.shape[-1]
+        _check_scores(weights, B, G, n, "weights")
+        _check_scores(weights_out, B, G, min(k_max, n), "weights_out")
+        if weights_out.shape[2] < k_max or weights_out.shape[1] < G:
+            raise ValueError(f"weights_out {tuple(weights_out.shape)} does not hold [{B}, {G}, {k_max}]")
+        ws = (weights.stride(0), weights.stride(1) if weights.shape[1] > 1 else 0, n, weights_out.stride(0),
+              weights_out.stride(1))
+    if new_lens is not None and (new_lens.dtype != torch.int32 or new_lens.numel() < B or not new_lens.is_contiguous()):
+        raise ValueError("new_lens must be a contiguous int32 [B] tensor")
+    what = "dustin_kv4_evict" if four else "dustin_kv_evict"
+    args = (*(ctypes.byref(x) for x in views), B, _ptr(idx), idx.stride(0), idx.stride(1), _ptr(count), G, k_max,
+            _ptr(weights), ws[0], ws[1], ws[2], _ptr(weights_out), ws[3], ws[4], _ptr(new_lens), _stream(stream))
+    keep = (k, v, k_out, v_out, idx, count, tables, views, weights, weights_out, new_lens)
+    return Call(getattr(lib(), what), args, what, keep, (k_out, v_out))
+
+
+def kv_evict(k, v, idx, count, **kw):
+    """The kept rows of a layer's caches to the front of others (or in place); returns (k_out, v_out)."""
+    return plan_kv_evict(k, v, idx, count, **kw)()

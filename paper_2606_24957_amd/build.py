@@ -9,7 +9,8 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libdustin.so")
 SOURCES = ["score_once_pair.hip", "score_once.hip", "api.hip", "attn.hip", "score.hip", "score_sync.hip",
-           "score_reread.hip", "topk.hip", "kv.hip", "page.hip", "arr.hip", "probe.hip"]
+           "score_reread.hip", "topk.hip", "kv.hip", "page.hip", "arr.hip", "probe.hip",
+           "api_kv4.hip", "kv4.hip", "evict.hip", "attn_kv4.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
@@ -22,7 +23,7 @@ FLAGS = ["--offload-arch=" + ARCH, "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-
 
 # The attention kernels are defined for finite Q/K/V only: without NaN semantics the
 # compiler drops the canonicalising moves it would put in front of every max.
-EXTRA = {"attn.hip": ["-fno-honor-nans"]}
+EXTRA = {"attn.hip": ["-fno-honor-nans"], "attn_kv4.hip": ["-fno-honor-nans"]}
 
 
 def _compile(src: str, verbose: bool) -> str:

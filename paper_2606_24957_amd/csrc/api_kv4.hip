@@ -1,0 +1,322 @@
+// api_kv4.hip -- the extern "C" boundary of the 4-bit cache (append, read, attention) and of eviction: argument
+// validation, workspace layout, launch configuration.  Validation happens before any HIP call.
+#include <math.h>
+
+#include "kv4.hpp"
+#include "validate.hpp"
+
+using namespace dustin;
+
+namespace {
+
+bool pages_ok(const int32_t* table, int page_size, int max_pages, int num_pages, int64_t stride_page, int* shift) {
+  if (page_size <= 0 || (page_size & (page_size - 1)) || max_pages <= 0 || num_pages <= 0 || stride_page <= 0 ||
+      !aligned(table, 4))
+    return false;
+  *shift = 0;
+  while ((1 << *shift) < page_size) ++*shift;
+  return true;
+}
+
+// Validates a 4-bit cache view for `need` addressable positions per sequence.
+dustin_status kv4_of(const dustin_kv4* kv, int64_t need, Kv4View* out) {
+  if (!kv || !kv->data || !kv->scales || kv->num_kv_heads <= 0) return DUSTIN_ERR_INVALID_ARG;
+  if (kv->head_dim != 64 && kv->head_dim != 128) return DUSTIN_ERR_UNSUPPORTED;
+  const int sb = kv->head_dim / kKv4Block;
+  if (!aligned(kv->data, 16) || kv->stride_b % 16 || kv->stride_n % 16 || kv->stride_h % 16 || kv->stride_page % 16 ||
+      !aligned(kv->scales, sb) || kv->scale_stride_b % sb || kv->scale_stride_n % sb || kv->scale_stride_h % sb ||
+      kv->scale_stride_page % sb)
+    return DUSTIN_ERR_INVALID_ARG;
+  if (kv->stride_n <= 0 || kv->stride_h < 0 || kv->stride_b < 0 || kv->scale_stride_n <= 0 || kv->scale_stride_h < 0 ||
+      kv->scale_stride_b < 0)
+    return DUSTIN_ERR_INVALID_ARG;
+  memset(out, 0, sizeof *out);
+  out->data = static_cast<const uint8_t*>(kv->data);
+  out->scales = static_cast<const uint8_t*>(kv->scales);
+  out->stride_b = kv->stride_b;
+  out->stride_n = kv->stride_n;
+  out->stride_h = kv->stride_h;
+  out->sstride_b = kv->scale_stride_b;
+  out->sstride_n = kv->scale_stride_n;
+  out->sstride_h = kv->scale_stride_h;
+  if (kv->page_table) {
+    if (!pages_ok(kv->page_table, kv->page_size, kv->max_pages, kv->num_pages, kv->stride_page, &out->page_shift) ||
+        kv->scale_stride_page <= 0)
+      return DUSTIN_ERR_INVALID_ARG;
+    out->page_table = kv->page_table;
+    out->max_pages = kv->max_pages;
+    out->num_pages = kv->num_pages;
+    out->stride_page = kv->stride_page;
+    out->sstride_page = kv->scale_stride_page;
+    out->capacity = (int64_t)kv->max_pages * kv->page_size;
+  } else {
+    out->capacity = kv->capacity;
+  }
+  if (out->capacity < need || out->capacity <= 0) return DUSTIN_ERR_INVALID_ARG;
+  if (out->capacity > INT32_MAX) return DUSTIN_ERR_UNSUPPORTED;
+  return DUSTIN_OK;
+}
+
+// K and V of one call: the same heads, channels and pages.
+template <class Kv>
+bool same_layout(const Kv* k, const Kv* v) {
+  return k->num_kv_heads == v->num_kv_heads && k->head_dim == v->head_dim && k->page_table == v->page_table &&
+         (!k->page_table ||
+          (k->page_size == v->page_size && k->max_pages == v->max_pages && k->num_pages == v->num_pages));
+}
+
+dustin_status kv4_rows(bool append, const void* k_rows, int64_t k_sb, int64_t k_st, int64_t k_sh, const void* v_rows,
+                       int64_t v_sb, int64_t v_st, int64_t v_sh, const dustin_kv4* k, const dustin_kv4* v,
+                       const dustin_batch* bt, void* stream) {
+  if (!batch_ok(bt) || !k_rows || !v_rows || !k || !v) return DUSTIN_ERR_INVALID_ARG;
+  if (!rows_aligned(k_rows, k_sb, k_st, k_sh) || !rows_aligned(v_rows, v_sb, v_st, v_sh)) return DUSTIN_ERR_INVALID_ARG;
+  if (!same_layout(k, v)) return DUSTIN_ERR_INVALID_ARG;
+  Kv4RowsArgs a;
+  memset(&a, 0, sizeof a);
+  const int64_t need = (int64_t)bt->max_len + bt->nq_max;
+  dustin_status st = kv4_of(k, need, &a.k);
+  if (st == DUSTIN_OK) st = kv4_of(v, need, &a.v);
+  if (st != DUSTIN_OK) return st;
+  if ((int64_t)bt->nq_max * k->num_kv_heads * (k->head_dim / 8) > INT32_MAX / 4) return DUSTIN_ERR_UNSUPPORTED;
+  a.k_in = static_cast<const uint16_t*>(k_rows);
+  a.v_in = static_cast<const uint16_t*>(v_rows);
+  a.k_out = const_cast<uint16_t*>(a.k_in);
+  a.v_out = const_cast<uint16_t*>(a.v_in);
+  a.k_sb = k_sb;
+  a.k_st = k_st;
+  a.k_sh = k_sh;
+  a.v_sb = v_sb;
+  a.v_st = v_st;
+  a.v_sh = v_sh;
+  a.dims = dims_of(bt);
+  a.batch = bt->batch;
+  a.num_kv_heads = k->num_kv_heads;
+  a.head_dim = k->head_dim;
+  const hipError_t e = append ? launch_kv4_append(a, static_cast<hipStream_t>(stream))
+                              : launch_kv4_read(a, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? DUSTIN_OK : DUSTIN_ERR_LAUNCH;
+}
+
+// ---- attention
+
+constexpr int kAttn4Units = 256;
+constexpr int64_t kAttn4MaxPairs = 65536;
+
+int attn4_row_tiles(int nq_max, int group_size) {
+  const int rt = (nq_max * group_size + 15) / 16;
+  return rt == 7 ? 8 : rt < 1 ? 1 : rt;  // instantiated tile counts: 1 to 6 and 8
+}
+
+// Workgroups of a call whose pairs hold up to `tokens` tokens, window included.
+int attn4_units(int64_t pairs, int64_t tokens) {
+  const int64_t most = pairs * ((tokens + kAttn4Granule - 1) / kAttn4Granule);
+  const int64_t cap = env_int("DUSTIN_KV4_UNITS", kAttn4Units);
+  const int64_t u = most < cap ? most : cap;
+  return (int)((u + 7) / 8 * 8);
+}
+
+size_t attn4_ws(int units, int64_t rows_max) {
+  return round_up((size_t)units * 2 * rows_max * 128 * sizeof(float), kAlign) +
+         round_up((size_t)units * 2 * rows_max * sizeof(float2), kAlign);
+}
+
+dustin_status attn4(bool sparse, const void* q, int64_t q_sb, int64_t q_st, int64_t q_sh, int32_t num_q_heads,
+                    const dustin_kv4* k, const dustin_kv4* v, const dustin_batch* bt, const int32_t* idx,
+                    int64_t idx_sb, int64_t idx_sg, const int32_t* count, int32_t groups, float scale, void* out,
+                    int64_t o_sb, int64_t o_st, int64_t o_sh, void* ws, size_t ws_bytes, void* stream) {
+  if (!batch_ok(bt) || !q || !out || !k || !v) return DUSTIN_ERR_INVALID_ARG;
+  if (!isfinite(scale) || !(scale > 0.f)) return DUSTIN_ERR_INVALID_ARG;
+  const int H = k->num_kv_heads;
+  if (num_q_heads <= 0 || H <= 0 || num_q_heads % H || !same_layout(k, v)) return DUSTIN_ERR_INVALID_ARG;
+  if (k->head_dim != 128) return DUSTIN_ERR_UNSUPPORTED;
+  if (bt->max_len > INT32_MAX - 1024) return DUSTIN_ERR_UNSUPPORTED;  // positions N_b + t are int32
+  if (!rows_aligned(q, q_sb, q_st, q_sh) || !rows_aligned(out, o_sb, o_st, o_sh)) return DUSTIN_ERR_INVALID_ARG;
+  const int gs = num_q_heads / H;
+  if ((int64_t)bt->nq_max * gs > 128) return DUSTIN_ERR_UNSUPPORTED;
+  const int64_t pairs = (int64_t)bt->batch * H;
+  if (pairs > kAttn4MaxPairs) return DUSTIN_ERR_UNSUPPORTED;
+  if (sparse) {
+    if (!idx || !count || (groups != 1 && groups != H)) return DUSTIN_ERR_INVALID_ARG;
+    if (!aligned(idx, 4) || !aligned(count, 4) || idx_sb < 0 || idx_sg < 0) return DUSTIN_ERR_INVALID_ARG;
+    if (bt->k_max > INT32_MAX - 1024) return DUSTIN_ERR_UNSUPPORTED;
+  }
+  Attn4Args a;
+  memset(&a, 0, sizeof a);
+  const int64_t need = (int64_t)bt->max_len + bt->nq_max;
+  dustin_status st = kv4_of(k, need, &a.k);
+  if (st == DUSTIN_OK) st = kv4_of(v, need, &a.v);
+  if (st != DUSTIN_OK) return st;
+  if (bt->batch == 0 || bt->nq_max == 0) return DUSTIN_OK;
+  a.q = static_cast<const uint16_t*>(q);
+  a.q_sb = q_sb;
+  a.q_st = q_st;
+  a.q_sh = q_sh;
+  a.out = static_cast<uint16_t*>(out);
+  a.o_sb = o_sb;
+  a.o_st = o_st;
+  a.o_sh = o_sh;
+  a.dims = dims_of(bt);
+  a.idx = idx;
+  a.idx_sb = idx_sb;
+  a.idx_sg = idx_sg;
+  a.count = count;
+  a.groups = sparse ? groups : 1;
+  a.num_kv_heads = H;
+  a.group_size = gs;
+  a.pairs = (int32_t)pairs;
+  a.scale_log2 = scale * kLog2e;
+  a.rows_max = bt->nq_max * gs;
+  a.units = attn4_units(pairs, (int64_t)(sparse ? bt->k_max : bt->max_len) + bt->nq_max);
+  a.min_granules = 1;
+  if (!ws || ws_bytes < attn4_ws(a.units, a.rows_max) || !aligned(ws, kAlign)) return DUSTIN_ERR_WORKSPACE;
+  a.part = static_cast<float*>(ws);
+  a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) +
+                                        round_up((size_t)a.units * 2 * a.rows_max * 128 * sizeof(float), kAlign));
+  const hipError_t e = launch_attn_kv4(a, attn4_row_tiles(bt->nq_max, gs), sparse, a.k.page_table != nullptr,
+                                       static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? DUSTIN_OK : DUSTIN_ERR_LAUNCH;
+}
+
+// ---- eviction
+
+dustin_status evict_cache(const dustin_kv* kv, int64_t need, EvictCache* out) {
+  if (!kv) return DUSTIN_ERR_INVALID_ARG;
+  if (kv->head_dim != 64 && kv->head_dim != 128) return DUSTIN_ERR_UNSUPPORTED;
+  KvView v;
+  const dustin_status st = kv_of(kv, kv->head_dim, need, &v);
+  if (st != DUSTIN_OK) return st;
+  if (v.capacity > INT32_MAX) return DUSTIN_ERR_UNSUPPORTED;
+  *out = EvictCache{reinterpret_cast<const uint8_t*>(v.data), nullptr, 2 * v.stride_b, 2 * v.stride_n, 2 * v.stride_h,
+                    2 * v.stride_page, 0, 0, 0, 0, v.page_table, v.page_shift, v.max_pages, v.num_pages,
+                    (int32_t)(v.capacity - 1)};
+  return DUSTIN_OK;
+}
+
+dustin_status evict_cache(const dustin_kv4* kv, int64_t need, EvictCache* out) {
+  Kv4View v;
+  const dustin_status st = kv4_of(kv, need, &v);
+  if (st != DUSTIN_OK) return st;
+  *out = EvictCache{v.data, v.scales, v.stride_b, v.stride_n, v.stride_h, v.stride_page, v.sstride_b, v.sstride_n,
+                    v.sstride_h, v.sstride_page, v.page_table, v.page_shift, v.max_pages, v.num_pages,
+                    (int32_t)(v.capacity - 1)};
+  return DUSTIN_OK;
+}
+
+// Equal caches of a call with `heads` KV heads and `batch` sequences (strides that no row uses aside).
+bool same_cache(const EvictCache& x, const EvictCache& y, int heads, int batch) {
+  if (x.data != y.data || x.scales != y.scales || x.page_table != y.page_table) return false;
+  if (x.stride_n != y.stride_n || x.sstride_n != y.sstride_n) return false;
+  if (heads > 1 && (x.stride_h != y.stride_h || x.sstride_h != y.sstride_h)) return false;
+  if (x.page_table)
+    return x.page_shift == y.page_shift && x.max_pages == y.max_pages && x.num_pages == y.num_pages &&
+           x.stride_page == y.stride_page && x.sstride_page == y.sstride_page;
+  return batch <= 1 || (x.stride_b == y.stride_b && x.sstride_b == y.sstride_b);
+}
+
+template <class Kv>
+dustin_status evict(const Kv* k, const Kv* v, const Kv* k_out, const Kv* v_out, int32_t batch, const int32_t* idx,
+                    int64_t idx_sb, int64_t idx_sg, const int32_t* count, int32_t groups, int32_t k_max, const float* w,
+                    int64_t w_sb, int64_t w_sg, int32_t w_len, float* w_out, int64_t wo_sb, int64_t wo_sg,
+                    int32_t* new_lens, int row_bytes_per_dim2, bool four, void* stream) {
+  if (!k || !v || !k_out || !v_out || batch < 0 || k_max < 0 || !idx || !count) return DUSTIN_ERR_INVALID_ARG;
+  if (!same_layout(k, v) || !same_layout(k_out, v_out) || k->num_kv_heads != k_out->num_kv_heads ||
+      k->head_dim != k_out->head_dim)
+    return DUSTIN_ERR_INVALID_ARG;
+  if (groups != 1 && groups != k->num_kv_heads) return DUSTIN_ERR_INVALID_ARG;
+  if (!aligned(idx, 4) || !aligned(count, 4) || !aligned(new_lens, 4) || idx_sb < 0 || idx_sg < 0)
+    return DUSTIN_ERR_INVALID_ARG;
+  if (!w != !w_out || !aligned(w, 4) || !aligned(w_out, 4)) return DUSTIN_ERR_INVALID_ARG;
+  if (w && (w_len <= 0 || w_sb < 0 || w_sg < 0 || wo_sb < 0 || wo_sg < 0)) return DUSTIN_ERR_INVALID_ARG;
+  EvictArgs a;
+  memset(&a, 0, sizeof a);
+  dustin_status st = evict_cache(k, 1, &a.src[0]);
+  if (st == DUSTIN_OK) st = evict_cache(v, 1, &a.src[1]);
+  if (st == DUSTIN_OK) st = evict_cache(k_out, k_max, &a.dst[0]);
+  if (st == DUSTIN_OK) st = evict_cache(v_out, k_max, &a.dst[1]);
+  if (st != DUSTIN_OK) return st;
+  const bool same_k = same_cache(a.src[0], a.dst[0], k->num_kv_heads, batch);
+  const bool same_v = same_cache(a.src[1], a.dst[1], k->num_kv_heads, batch);
+  if (same_k != same_v || (!same_k && (k->data == k_out->data || v->data == v_out->data))) return DUSTIN_ERR_INVALID_ARG;
+  if (batch == 0) return DUSTIN_OK;
+  a.idx = idx;
+  a.idx_sb = idx_sb;
+  a.idx_sg = idx_sg;
+  a.count = count;
+  a.w = w;
+  a.w_out = w_out;
+  a.w_sb = w_sb;
+  a.w_sg = w_sg;
+  a.wo_sb = wo_sb;
+  a.wo_sg = wo_sg;
+  a.new_lens = new_lens;
+  a.batch = batch;
+  a.groups = groups;
+  a.num_kv_heads = k->num_kv_heads;
+  a.k_max = k_max;
+  a.w_len = w_len;
+  a.row_bytes = k->head_dim * row_bytes_per_dim2 / 2;
+  a.scale_bytes = four ? k->head_dim / kKv4Block : 0;
+  a.in_place = same_k;
+  return launch_evict(a, static_cast<hipStream_t>(stream)) == hipSuccess ? DUSTIN_OK : DUSTIN_ERR_LAUNCH;
+}
+
+}  // namespace
+
+extern "C" {
+
+dustin_status dustin_kv4_append(const void* k_new, int64_t k_sb, int64_t k_st, int64_t k_sh, const void* v_new,
+                                int64_t v_sb, int64_t v_st, int64_t v_sh, const dustin_kv4* k, const dustin_kv4* v,
+                                const dustin_batch* bt, void* stream) {
+  return kv4_rows(true, k_new, k_sb, k_st, k_sh, v_new, v_sb, v_st, v_sh, k, v, bt, stream);
+}
+
+dustin_status dustin_kv4_read(void* k_out, int64_t k_sb, int64_t k_st, int64_t k_sh, void* v_out, int64_t v_sb,
+                              int64_t v_st, int64_t v_sh, const dustin_kv4* k, const dustin_kv4* v,
+                              const dustin_batch* bt, void* stream) {
+  return kv4_rows(false, k_out, k_sb, k_st, k_sh, v_out, v_sb, v_st, v_sh, k, v, bt, stream);
+}
+
+size_t dustin_attn_kv4_workspace(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t nq_max,
+                                 int32_t max_tokens) {
+  if (batch <= 0 || num_kv_heads <= 0 || num_q_heads <= 0 || num_q_heads % num_kv_heads || nq_max <= 0 || max_tokens < 0)
+    return 0;
+  return attn4_ws(attn4_units((int64_t)batch * num_kv_heads, (int64_t)max_tokens + nq_max),
+                  (int64_t)nq_max * (num_q_heads / num_kv_heads));
+}
+
+dustin_status dustin_sparse_verify_attn_kv4(const void* q, int64_t q_sb, int64_t q_st, int64_t q_sh,
+                                            int32_t num_q_heads, const dustin_kv4* k, const dustin_kv4* v,
+                                            const dustin_batch* bt, const int32_t* idx, int64_t idx_sb, int64_t idx_sg,
+                                            const int32_t* count, int32_t groups, float scale, void* out, int64_t o_sb,
+                                            int64_t o_st, int64_t o_sh, void* workspace, size_t workspace_bytes,
+                                            void* stream) {
+  return attn4(true, q, q_sb, q_st, q_sh, num_q_heads, k, v, bt, idx, idx_sb, idx_sg, count, groups, scale, out, o_sb,
+               o_st, o_sh, workspace, workspace_bytes, stream);
+}
+
+dustin_status dustin_dense_verify_attn_kv4(const void* q, int64_t q_sb, int64_t q_st, int64_t q_sh,
+                                           int32_t num_q_heads, const dustin_kv4* k, const dustin_kv4* v,
+                                           const dustin_batch* bt, float scale, void* out, int64_t o_sb, int64_t o_st,
+                                           int64_t o_sh, void* workspace, size_t workspace_bytes, void* stream) {
+  return attn4(false, q, q_sb, q_st, q_sh, num_q_heads, k, v, bt, nullptr, 0, 0, nullptr, 1, scale, out, o_sb, o_st,
+               o_sh, workspace, workspace_bytes, stream);
+}
+
+dustin_status dustin_kv_evict(const dustin_kv* k, const dustin_kv* v, const dustin_kv* k_out, const dustin_kv* v_out,
+                              int32_t batch, const int32_t* idx, int64_t idx_sb, int64_t idx_sg, const int32_t* count,
+                              int32_t groups, int32_t k_max, const float* w, int64_t w_sb, int64_t w_sg, int32_t w_len,
+                              float* w_out, int64_t wo_sb, int64_t wo_sg, int32_t* new_lens, void* stream) {
+  return evict(k, v, k_out, v_out, batch, idx, idx_sb, idx_sg, count, groups, k_max, w, w_sb, w_sg, w_len, w_out, wo_sb,
+               wo_sg, new_lens, 4, false, stream);
+}
+
+dustin_status dustin_kv4_evict(const dustin_kv4* k, const dustin_kv4* v, const dustin_kv4* k_out,
+                               const dustin_kv4* v_out, int32_t batch, const int32_t* idx, int64_t idx_sb,
+                               int64_t idx_sg, const int32_t* count, int32_t groups, int32_t k_max, const float* w,
+                               int64_t w_sb, int64_t w_sg, int32_t w_len, float* w_out, int64_t wo_sb, int64_t wo_sg,
+                               int32_t* new_lens, void* stream) {
+  return evict(k, v, k_out, v_out, batch, idx, idx_sb, idx_sg, count, groups, k_max, w, w_sb, w_sg, w_len, w_out, wo_sb,
+               wo_sg, new_lens, 1, true, stream);
+}
+
+}  // extern "C"

@@ -102,11 +102,6 @@ dustin_status kv4_rows(bool append, const void* k_rows, int64_t k_sb, int64_t k_
 constexpr int kAttn4Units = 256;
 constexpr int64_t kAttn4MaxPairs = 65536;
 
-int attn4_row_tiles(int nq_max, int group_size) {
-  const int rt = (nq_max * group_size + 15) / 16;
-  return rt == 7 ? 8 : rt < 1 ? 1 : rt;  // instantiated tile counts: 1 to 6 and 8
-}
-
 // Workgroups of a call whose pairs hold up to `tokens` tokens, window included.
 int attn4_units(int64_t pairs, int64_t tokens) {
   const int64_t most = pairs * ((tokens + kAttn4Granule - 1) / kAttn4Granule);
@@ -115,9 +110,16 @@ int attn4_units(int64_t pairs, int64_t tokens) {
   return (int)((u + 7) / 8 * 8);
 }
 
-size_t attn4_ws(int units, int64_t rows_max) {
-  return round_up((size_t)units * 2 * rows_max * 128 * sizeof(float), kAlign) +
-         round_up((size_t)units * 2 * rows_max * sizeof(float2), kAlign);
+// Workspace: the plan, then the parts of every run.
+struct Attn4Ws {
+  size_t ml, acc, total;
+};
+Attn4Ws attn4_ws(int64_t pairs, int units, int64_t rows_max) {
+  Attn4Ws w;
+  w.ml = round_up((size_t)(pairs + 1) * sizeof(int32_t), kAlign);
+  w.acc = w.ml + round_up((size_t)units * 2 * rows_max * sizeof(float2), kAlign);
+  w.total = w.acc + round_up((size_t)units * 2 * rows_max * 128 * sizeof(float), kAlign);
+  return w;
 }
 
 dustin_status attn4(bool sparse, const void* q, int64_t q_sb, int64_t q_st, int64_t q_sh, int32_t num_q_heads,
@@ -146,6 +148,12 @@ dustin_status attn4(bool sparse, const void* q, int64_t q_sb, int64_t q_st, int6
   dustin_status st = kv4_of(k, need, &a.k);
   if (st == DUSTIN_OK) st = kv4_of(v, need, &a.v);
   if (st != DUSTIN_OK) return st;
+  // the kernels multiply positions and pages by 32-bit strides, and count granules in 32 bits
+  for (const Kv4View* c : {&a.k, &a.v})
+    for (const int64_t x : {c->stride_n, c->sstride_n, c->stride_page, c->sstride_page})
+      if (x > (int64_t)UINT32_MAX) return DUSTIN_ERR_UNSUPPORTED;
+  const int64_t tokens = (int64_t)(sparse ? bt->k_max : bt->max_len) + bt->nq_max;
+  if (pairs * ((tokens + kAttn4Granule - 1) / kAttn4Granule) > INT32_MAX) return DUSTIN_ERR_UNSUPPORTED;
   if (bt->batch == 0 || bt->nq_max == 0) return DUSTIN_OK;
   a.q = static_cast<const uint16_t*>(q);
   a.q_sb = q_sb;
@@ -166,13 +174,17 @@ dustin_status attn4(bool sparse, const void* q, int64_t q_sb, int64_t q_st, int6
   a.pairs = (int32_t)pairs;
   a.scale_log2 = scale * kLog2e;
   a.rows_max = bt->nq_max * gs;
-  a.units = attn4_units(pairs, (int64_t)(sparse ? bt->k_max : bt->max_len) + bt->nq_max);
+  a.units = attn4_units(pairs, tokens);
   a.min_granules = 1;
-  if (!ws || ws_bytes < attn4_ws(a.units, a.rows_max) || !aligned(ws, kAlign)) return DUSTIN_ERR_WORKSPACE;
-  a.part = static_cast<float*>(ws);
-  a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) +
-                                        round_up((size_t)a.units * 2 * a.rows_max * 128 * sizeof(float), kAlign));
-  const hipError_t e = launch_attn_kv4(a, attn4_row_tiles(bt->nq_max, gs), sparse, a.k.page_table != nullptr,
+  const Attn4Ws w = attn4_ws(pairs, a.units, a.rows_max);
+  if (!ws || ws_bytes < w.total || !aligned(ws, kAlign)) return DUSTIN_ERR_WORKSPACE;
+  char* base = static_cast<char*>(ws);
+  a.plan = reinterpret_cast<int32_t*>(base);
+  a.part_ml = reinterpret_cast<float2*>(base + w.ml);
+  a.part = reinterpret_cast<float*>(base + w.acc);
+  if (sparse && bt->k_max == 0) a.idx = bt->seq_lens, a.idx_sb = a.idx_sg = 0;  // no entries: read, and not used
+  a.idx_last = sparse && bt->k_max > 0 ? bt->k_max - 1 : 0;
+  const hipError_t e = launch_attn_kv4(a, (a.rows_max + 15) / 16, sparse, a.k.page_table != nullptr,
                                        static_cast<hipStream_t>(stream));
   return e == hipSuccess ? DUSTIN_OK : DUSTIN_ERR_LAUNCH;
 }
@@ -280,8 +292,8 @@ size_t dustin_attn_kv4_workspace(int32_t batch, int32_t num_q_heads, int32_t num
                                  int32_t max_tokens) {
   if (batch <= 0 || num_kv_heads <= 0 || num_q_heads <= 0 || num_q_heads % num_kv_heads || nq_max <= 0 || max_tokens < 0)
     return 0;
-  return attn4_ws(attn4_units((int64_t)batch * num_kv_heads, (int64_t)max_tokens + nq_max),
-                  (int64_t)nq_max * (num_q_heads / num_kv_heads));
+  const int64_t pairs = (int64_t)batch * num_kv_heads;
+  return attn4_ws(pairs, attn4_units(pairs, (int64_t)max_tokens + nq_max), (int64_t)nq_max * (num_q_heads / num_kv_heads)).total;
 }
 
 dustin_status dustin_sparse_verify_attn_kv4(const void* q, int64_t q_sb, int64_t q_st, int64_t q_sh,

@@ -1,16 +1,17 @@
 // attn_kv4.hip -- verification attention over a 4-bit cache for gfx950: over the selected positions (sparse) or every
 // committed one (dense), both followed by the causal verification window.
 //
-// A workgroup of four waves takes an equal share of the batch's tokens: the tokens of all (sequence, KV head) pairs
+// A workgroup of eight waves takes an equal share of the batch's tokens: the tokens of all (sequence, KV head) pairs
 // lie end to end on one axis, in granules of 128, which is cut into as many equal runs as there are workgroups.  A run
 // may end inside a pair, or span several; the parts of a pair that several workgroups hold are joined by a second
-// kernel.  Within a part the waves take 32-token steps in turn:
-//   K     lane (token, block) loads a block's 16 bytes, and turns them into four bf16 operands of the score product;
-//         the channels of a 32-channel step are those of four blocks, and the queries are laid out to match
-//   V     loads in the same way; its bf16 rows go to a wave's LDS tile, from where transpose loads take the value
-//         product's operands
-//   S^T = K Q^T, softmax with a lazy running maximum, O^T += V^T P^T, as in the attention over a bf16 cache.
-// Two steps' rows are in flight in registers while a third is computed.
+// kernel.  A part is done in rounds, of 32 tokens to a wave (16 from two tiles of query rows on):
+//   loads  a wave's rows of the rounds ahead go from memory straight into LDS as they are, 136 bytes a token
+//   S      the wave decodes its tokens' K rows into MFMA operands (lane: token, block; the channels of one 32-channel
+//          step are those of four blocks, and the queries are laid out to match): S^T = K Q^T for its tokens, all rows
+//   P      probabilities against a running reference of each row, the same in all waves, as operands of the value
+//          product into LDS; and its tokens' V rows, decoded, into a tile that all waves share
+//   O      after a barrier each wave adds all the round's tokens to 16 of the 128 channels: O^T += V^T P^T
+// so that a wave holds an eighth of the accumulator, and nothing is left to add up at the end but the row sums.
 #include "kv4.hpp"
 
 namespace dustin {
@@ -18,13 +19,56 @@ namespace dustin {
 namespace {
 
 constexpr int kD4 = 128;
-constexpr int kW4 = 4;
-constexpr int kStep4 = 32;
-constexpr float kRescale4 = 8.f;  // lazy rescale threshold (log2)
+constexpr int kW4 = 8;                   // waves of a workgroup: two to a SIMD
+constexpr int kThreads4 = kW4 * kWave;
+constexpr float kRescale4 = 8.f;         // the references move when a row's maximum passes its own by 2^8
+constexpr float kNoRef = -3e38f;         // reference of a row that has seen no token: any score passes it
+constexpr int kRing4 = 8;                // rounds whose positions and pages a wave holds
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef short v4i16 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) void lds_void4;
+
+// Loads straight into LDS: lane l's 16 (or 4) bytes go to lds + 16 l (4 l).
+__device__ __forceinline__ void dma16(const uint8_t* src, char* lds) {
+  __builtin_amdgcn_global_load_lds(src, (lds_void4*)lds, 16, 0, 0);
+}
+__device__ __forceinline__ void dma4(const void* src, char* lds) {
+  __builtin_amdgcn_global_load_lds(src, (lds_void4*)lds, 4, 0, 0);
+}
+__device__ __forceinline__ uint32_t lds_addr(const void* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
+}
+// Waits until only the last n of the wave's loads may be outstanding.
+template <int n>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((n & 15) | ((n >> 4) << 14) | 0x0F70);
+  asm volatile("" ::: "memory");
+}
+// A barrier that waits for the wave's LDS instructions but not for its loads.
+__device__ __forceinline__ void lds_barrier4() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+// Words of a ring.  (In assembly with its wait: a plain read would wait for every load in flight into LDS.)
+__device__ __forceinline__ int read_word(uint32_t x) {
+  int u;
+  asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(u) : "v"(x) : "memory");
+  return u;
+}
+template <int n>
+__device__ __forceinline__ void read_words(const uint32_t (&x)[n], int (&u)[n]) {
+  if constexpr (n == 2)
+    asm volatile("ds_read_b32 %0, %2\n\tds_read_b32 %1, %3\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(u[0]), "=&v"(u[1]) : "v"(x[0]), "v"(x[1]) : "memory");
+  else
+    asm volatile("ds_read_b32 %0, %3\n\tds_read_b32 %1, %4\n\tds_read_b32 %2, %5\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(u[0]), "=&v"(u[1]), "=&v"(u[2]) : "v"(x[0]), "v"(x[1]), "v"(x[2]) : "memory");
+}
 
 __device__ __forceinline__ u32x2 read_tr16(const char* p) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
@@ -35,128 +79,228 @@ __device__ __forceinline__ uint32_t pk_bf16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
 }
 
-// The run of granules of each workgroup: `first` granules of pair p, and the length of a run.
-struct Plan4 {
-  int64_t total, per;
+// floor(a / b) for 0 <= a < 2^22, 1 <= b < 2^22: the reciprocal's estimate is within one of it.
+__device__ __forceinline__ int div22(int a, int b) {
+  int q = (int)((float)a * __builtin_amdgcn_rcpf((float)b));
+  q -= (int)__umul24((unsigned)q, (unsigned)b) > a ? 1 : 0;
+  q += (int)__umul24((unsigned)(q + 1), (unsigned)b) <= a ? 1 : 0;
+  return q;
+}
+
+// Inclusive sum over a wave (row shifts, then the rows' last lanes broadcast).
+__device__ __forceinline__ int wave_sum_incl(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+  return v;
+}
+
+// The sizes of a pair: window tokens, and tokens before them.
+struct Pair4 {
+  int T, body;
+  __device__ __forceinline__ int granules() const {
+    return T ? (body + T + kAttn4Granule - 1) / kAttn4Granule : 0;
+  }
 };
 
-__device__ __forceinline__ int granules_of(const Attn4Args& a, bool sparse, int pair) {
-  const int b = pair / a.num_kv_heads, g = pair - b * a.num_kv_heads;
-  const int T = a.dims.nq(b);
-  if (T == 0) return 0;
-  const int body = sparse ? clampi(a.count[b * a.groups + (a.groups == 1 ? 0 : g)], 0, a.dims.k_max) : a.dims.len(b);
-  return (body + T + kAttn4Granule - 1) / kAttn4Granule;
+template <bool kSparse>
+__device__ __forceinline__ Pair4 pair_of(const Attn4Args& a, int pair) {
+  const int b = div22(pair, a.num_kv_heads);
+  int body = 0;
+  if constexpr (kSparse) body = a.count[a.groups == 1 ? b : pair];
+  else body = a.dims.seq_lens[b];
+  return {a.dims.nq(b), clampi(body, 0, kSparse ? a.dims.k_max : a.dims.max_len)};
 }
 
-// Every thread sums the granules of a run of pairs; the sums before it and in all.
-__device__ __forceinline__ void scan_pairs(const Attn4Args& a, bool sparse, int64_t* sm, int& p0, int& p1, int64_t& before,
-                                           int64_t& total) {
-  const int per = (a.pairs + kW4 * kWave - 1) / (kW4 * kWave);
-  p0 = min(a.pairs, (int)threadIdx.x * per);
-  p1 = min(a.pairs, p0 + per);
-  int64_t own = 0;
-  for (int p = p0; p < p1; ++p) own += granules_of(a, sparse, p);
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-  int64_t incl = own;
-#pragma unroll
-  for (int d = 1; d < kWave; d *= 2) {
-    const int64_t y = __shfl_up(incl, d);
-    if (lane >= d) incl += y;
-  }
-  if (lane == kWave - 1) sm[wave] = incl;
-  __syncthreads();
-  int64_t base = 0;
-  total = 0;
-#pragma unroll
-  for (int w = 0; w < kW4; ++w) {
-    if (w < wave) base += sm[w];
-    total += sm[w];
-  }
-  before = base + incl - own;
-}
-
-__device__ __forceinline__ int64_t run_length(const Attn4Args& a, int64_t total) {
-  const int64_t per = (total + a.units - 1) / a.units;
+__device__ __forceinline__ int run_length(const Attn4Args& a, int total) {
+  const int per = (int)(((int64_t)total + a.units - 1) / a.units);
   return per < a.min_granules ? a.min_granules : per;
 }
 
 template <int RT, bool kSparse, bool kPaged>
-__global__ __launch_bounds__(kW4 * kWave) void attn_kv4_kernel(Attn4Args a) {
-  constexpr int NDT = kD4 / 16;
+__global__ __launch_bounds__(kThreads4) void attn_kv4_kernel(Attn4Args a) {
+  constexpr int kTpw = RT == 1 ? 32 : 16;        // tokens of a wave's round
+  constexpr int NT = kTpw / 16;
+  constexpr int kTok = kW4 * kTpw;               // of a round
+  constexpr int kRaw = kTpw * 136;               // a wave's rows and scales of a round as they come from memory
+  constexpr int kRawLoads = 2 * NT + 1;
+  constexpr int kSlots = RT == 1 || RT > 6 ? 2 : 3;        // rounds in flight
+  constexpr int kExtra = (kSparse ? 1 : 0) + (kPaged ? 1 : 0);  // loads of positions and pages in a round
+  constexpr bool kQReg = RT <= 6;                // the queries in registers, else read from LDS in every round
   constexpr int kQPitch = kD4 + 8;
-  constexpr int kPitch = kD4 + 4;
-  constexpr bool kQReg = RT <= 3;
-  constexpr int kVTile = kStep4 * kD4 * 2;
-  constexpr int kBuf = RT * 16 * kPitch;  // one wave's accumulator, floats
-  constexpr int kTiles = kW4 * kVTile;
-  constexpr int kNB = RT <= 4 ? 2 : 1;    // of them in LDS
-  constexpr int kFinal = kNB * kBuf * 4;
-  __shared__ __attribute__((aligned(1024))) char smem[kTiles > kFinal ? kTiles : kFinal];
-  __shared__ __attribute__((aligned(16))) uint16_t sm_q[RT * 16 * kQPitch];
-  __shared__ float sm_m[kW4][RT * 16], sm_l[kW4][RT * 16];
-  __shared__ int64_t sm_scan[kW4];
-  __shared__ int64_t sm_first[2];
+  constexpr int kQBytes = RT * 16 * kQPitch * 2;
+  constexpr int kVBytes = kTok * kD4 * 2;
+  // (objects of their own: the loads in flight into one then hold back no read of another)
+  __shared__ __attribute__((aligned(1024))) char sm_v[kVBytes > kQBytes || !kQReg ? kVBytes : kQBytes];
+  __shared__ __attribute__((aligned(16))) char sm_q_own[kQReg ? 16 : kQBytes];
+  __shared__ __attribute__((aligned(16))) char sm_p[RT * kTok * 32];  // [row tile][32 tokens][lane] of 16 bytes
+  __shared__ __attribute__((aligned(1024))) char sm_raw[kW4 * kSlots * kRaw];
+  __shared__ __attribute__((aligned(16))) char sm_pos[kSparse ? kW4 * kRing4 * kTpw * 4 : 16];
+  __shared__ __attribute__((aligned(16))) char sm_page[kPaged ? kW4 * kRing4 * kTpw * 4 : 16];
+  __shared__ __attribute__((aligned(16))) int sm_over[2][kW4];
+  __shared__ float sm_max[kW4][RT * 16];
+  __shared__ int sm_scan[kW4];
+  __shared__ int sm_first[2];
 
   const int lane = threadIdx.x & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int lr = lane & 15, lg = lane >> 4;
-  char* const vtile = smem + wave * kVTile;
+  char* const raw = sm_raw + wave * kSlots * kRaw;
+  char* const pos_ring = sm_pos + (kSparse ? wave * kRing4 * kTpw * 4 : 0);
+  char* const page_ring = sm_page + (kPaged ? wave * kRing4 * kTpw * 4 : 0);
 
-  int64_t total_g, before;
-  int p0, p1;
-  scan_pairs(a, kSparse, sm_scan, p0, p1, before, total_g);
-  const int64_t per = run_length(a, total_g);
-  const int64_t active = (total_g + per - 1) / per;  // runs there are
+  // ---- the workgroup's run of granules: every thread sums those of a few pairs
+  const int ppt = (a.pairs + kThreads4 - 1) / kThreads4;
+  const int p0 = min(a.pairs, (int)threadIdx.x * ppt), p1 = min(a.pairs, p0 + ppt);
+  int own = 0;
+  for (int p = p0; p < p1; ++p) own += pair_of<kSparse>(a, p).granules();
+  const int incl = wave_sum_incl(own);
+  if (lane == kWave - 1) sm_scan[wave] = incl;
+  lds_barrier4();
+  int total_g = 0, before = incl - own;
+#pragma unroll
+  for (int w = 0; w < kW4; ++w) {
+    const int x = sm_scan[w];
+    before += w < wave ? x : 0;
+    total_g += x;
+  }
+  total_g = __builtin_amdgcn_readfirstlane(total_g);
+  const int per = run_length(a, total_g);
+  const int active = (total_g + per - 1) / per;  // runs there are
   // consecutive runs on one XCD: workgroups go to the XCDs in turn
   const int xcd = blockIdx.x & 7;
-  const int64_t unit = (xcd * active + 7) / 8 + (blockIdx.x >> 3);
+  const int unit = (xcd * active + 7) / 8 + (blockIdx.x >> 3);
   if (unit >= ((xcd + 1) * active + 7) / 8) return;
-  const int64_t start = unit * per, end = start + per < total_g ? start + per : total_g;
+  const int start = unit * per, end = min(total_g, start + per);
   for (int p = p0; p < p1; ++p) {
-    const int n = granules_of(a, kSparse, p);
+    const int n = ppt == 1 ? own : pair_of<kSparse>(a, p).granules();
     if (before <= start && start < before + n) {
       sm_first[0] = p;
       sm_first[1] = before;
     }
     before += n;
   }
-  __syncthreads();
-  int pair = (int)sm_first[0];
-  int64_t pair_g = sm_first[1];  // its first granule
+  lds_barrier4();
+  int pair = __builtin_amdgcn_readfirstlane(sm_first[0]);
+  int pair_g = __builtin_amdgcn_readfirstlane(sm_first[1]);  // its first granule
+  if (unit == 0 && threadIdx.x == 0) a.plan[0] = per;
 
-  for (int64_t g0 = start; g0 < end; ++pair) {
-    const int n_g = granules_of(a, kSparse, pair);
+  for (int g0 = start; g0 < end; ++pair) {
+    const int b = div22(pair, a.num_kv_heads), g = pair - b * a.num_kv_heads;
+    const Pair4 pr = pair_of<kSparse>(a, pair);
+    const int N = a.dims.len(b);
+    const int n_g = pr.granules();
     if (n_g == 0) continue;
-    const int64_t pair_end = pair_g + n_g;
-    const int64_t g1 = pair_end < end ? pair_end : end;
-    const int b = pair / a.num_kv_heads, g = pair - b * a.num_kv_heads, gi = a.groups == 1 ? 0 : g;
-    const int N = a.dims.len(b), T = a.dims.nq(b);
-    const int wstart = kSparse ? clampi(a.count[b * a.groups + gi], 0, a.dims.k_max) : N;
-    const int total = wstart + T, rows = T * a.group_size;
-    const int nsteps = (total + kStep4 - 1) / kStep4;
-    const int s_begin = (int)(g0 - pair_g) * 4, s_end = min(nsteps, (int)(g1 - pair_g) * 4);
-    const int32_t* idx_row = kSparse ? a.idx + b * a.idx_sb + gi * a.idx_sg : nullptr;
-    const int cap_m1 = (int)(a.k.capacity - 1 < INT32_MAX ? a.k.capacity - 1 : INT32_MAX);
-    const uint8_t* kdata = a.k.data + g * a.k.stride_h + 16 * lg;
-    const uint8_t* vdata = a.v.data + g * a.v.stride_h + 16 * lg;
-    const uint8_t* kscale = a.k.scales + g * a.k.sstride_h + lg;
-    const uint8_t* vscale = a.v.scales + g * a.v.sstride_h + lg;
+    const int pair_end = pair_g + n_g;
+    const int g1 = min(pair_end, end);
+    const int T = pr.T, wstart = pr.body, total = wstart + T, rows = T * a.group_size;
+    const int t_begin = (g0 - pair_g) * kAttn4Granule, t_end = min(total, (g1 - pair_g) * kAttn4Granule);
+    if (g0 == pair_g && threadIdx.x == 0) a.plan[1 + pair] = pair_g;
+    const int32_t* idx_row = kSparse ? a.idx + b * a.idx_sb + (a.groups == 1 ? 0 : g) * a.idx_sg : nullptr;
+    const int cap_m1 = (int)(a.k.capacity - 1);
+    const uint8_t* kdata = a.k.data + g * a.k.stride_h + (kPaged ? 0 : b * a.k.stride_b) + 16 * lg;
+    const uint8_t* vdata = a.v.data + g * a.v.stride_h + (kPaged ? 0 : b * a.v.stride_b) + 16 * lg;
+    // scales: the first kTpw lanes take K's, the next V's
+    const bool v_lane = lane & kTpw;
+    const uint8_t* sdata = v_lane ? a.v.scales + g * a.v.sstride_h + (kPaged ? 0 : b * a.v.sstride_b)
+                                  : a.k.scales + g * a.k.sstride_h + (kPaged ? 0 : b * a.k.sstride_b);
+    const uint32_t s_sp = (uint32_t)(v_lane ? a.v.sstride_page : a.k.sstride_page);
+    const uint32_t s_sn = (uint32_t)(v_lane ? a.v.sstride_n : a.k.sstride_n);
 
-    // queries, absent rows as zeros
-    __syncthreads();  // the LDS of the part before is free
-    for (int e = threadIdx.x; e < RT * 16 * (kD4 / 8); e += kW4 * kWave) {
+    // ---- A round's rows pass three stages, each a load into LDS: the selected positions, their pages, the rows with
+    // their scales.  A token past the end is the last one, so every address is a row's.
+    auto ring_of = [&](int n) { return (n & (kRing4 - 1)) * kTpw * 4; };
+    auto token = [&](int n, int j) { return min(t_begin + n * kTok + wave * kTpw + j, total - 1); };
+    auto load_pos = [&](int n) {
+      if constexpr (kSparse)
+        if (lane < kTpw) dma4(idx_row + min(token(n, lane), a.idx_last), pos_ring + ring_of(n));
+    };
+    auto position = [&](int v, int sel) {
+      return clampi(v < wstart ? (kSparse ? sel : v) : N + (v - wstart), 0, cap_m1);
+    };
+    auto load_page = [&](int n) {
+      if constexpr (kPaged)
+        if (lane < kTpw) {
+          const int sel = kSparse ? read_word(lds_addr(pos_ring) + ring_of(n) + 4 * lane) : 0;
+          dma4(a.k.page_table + (int64_t)b * a.k.max_pages + (position(token(n, lane), sel) >> a.k.page_shift),
+               page_ring + ring_of(n));
+        }
+    };
+    // (strides below 2^32: the host checks)
+    auto offset = [&](int page, int slot, uint32_t sp, uint32_t sn) {
+      const uint64_t o = (uint64_t)(uint32_t)slot * sn;
+      return kPaged ? o + (uint64_t)(uint32_t)page * sp : o;
+    };
+    auto load_rows = [&](int n, int slot_n) {
+      char* const to = raw + slot_n * kRaw;
+      int j[NT + 1], page[NT + 1], slot[NT + 1];  // tokens of this lane's rows, and of its scale
+#pragma unroll
+      for (int i = 0; i < NT; ++i) j[i] = 16 * i + lr;
+      j[NT] = lane & (kTpw - 1);
+      int sel[NT + 1];
+      uint32_t at[NT + 1];
+#pragma unroll
+      for (int i = 0; i <= NT; ++i) sel[i] = page[i] = 0;
+      if constexpr (kSparse) {
+#pragma unroll
+        for (int i = 0; i <= NT; ++i) at[i] = lds_addr(pos_ring) + ring_of(n) + 4 * j[i];
+        read_words(at, sel);
+      }
+      if constexpr (kPaged) {
+#pragma unroll
+        for (int i = 0; i <= NT; ++i) at[i] = lds_addr(page_ring) + ring_of(n) + 4 * j[i];
+        read_words(at, page);
+      }
+#pragma unroll
+      for (int i = 0; i <= NT; ++i) {
+        slot[i] = position(token(n, j[i]), sel[i]);
+        if constexpr (kPaged) {
+          page[i] = clampi(page[i], 0, a.k.num_pages - 1);
+          slot[i] &= (1 << a.k.page_shift) - 1;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < NT; ++i) {
+        dma16(kdata + offset(page[i], slot[i], (uint32_t)a.k.stride_page, (uint32_t)a.k.stride_n), to + i * 1024);
+        dma16(vdata + offset(page[i], slot[i], (uint32_t)a.v.stride_page, (uint32_t)a.v.stride_n),
+              to + kTpw * 64 + i * 1024);
+      }
+      if (lane < 2 * kTpw) dma4(sdata + offset(page[NT], slot[NT], s_sp, s_sn), to + kTpw * 128);
+    };
+    if constexpr (kSparse) {
+#pragma unroll
+      for (int n = 0; n < kSlots + 4; ++n) load_pos(n);
+    }
+    // ---- queries, absent rows as zeros
+    char* const sm_q = kQReg ? sm_v : sm_q_own;
+    lds_barrier4();  // the LDS of the part before is free
+    for (int e = threadIdx.x; e < RT * 16 * (kD4 / 8); e += kThreads4) {
       const int r = e / (kD4 / 8), c0 = (e % (kD4 / 8)) * 8;
       u32x4 x = {0u, 0u, 0u, 0u};
       if (r < rows) {
-        const int t = r / a.group_size, hh = r - t * a.group_size;
+        const int t = div22(r, a.group_size), hh = r - t * a.group_size;
         x = load16(a.q + b * a.q_sb + t * a.q_st + (g * a.group_size + hh) * a.q_sh + c0);
       }
-      *reinterpret_cast<u32x4*>(sm_q + r * kQPitch + c0) = x;
+      *reinterpret_cast<u32x4*>(sm_q + (r * kQPitch + c0) * 2) = x;
     }
-    __syncthreads();
+    if constexpr (kSparse) wait_loads<0>();
+    if constexpr (kPaged) {
+#pragma unroll
+      for (int n = 0; n < kSlots + 2; ++n) load_page(n);
+      wait_loads<0>();
+    }
+#pragma unroll
+    for (int n = 0; n < kSlots; ++n) load_rows(n, n);
+    lds_barrier4();
+    // (the first round's rows: no loads of positions or pages lie between it and those behind, as the loop's wait
+    // counts them)
+    if constexpr (kExtra > 0) wait_loads<(kSlots - 1) * kRawLoads>();
     // Q^T as B operands: lane (row lr, block lg), operand ks: channels 32 lg + 8 ks + e
     auto read_q = [&](int rt, int ks) {
-      return as_bf16x8(*reinterpret_cast<const u32x4*>(sm_q + (rt * 16 + lr) * kQPitch + 32 * lg + 8 * ks));
+      return as_bf16x8(*reinterpret_cast<const u32x4*>(sm_q + ((rt * 16 + lr) * kQPitch + 32 * lg + 8 * ks) * 2));
     };
     bf16x8 qreg[kQReg ? RT : 1][4];
     if constexpr (kQReg)
@@ -165,222 +309,200 @@ __global__ __launch_bounds__(kW4 * kWave) void attn_kv4_kernel(Attn4Args a) {
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) qreg[rt][ks] = read_q(rt, ks);
     int limit[RT];  // token v is visible to this lane's row iff v <= limit
-    float m_ref[RT];
-    f32x4 acc[RT][NDT], accl[RT];
+    float m_ref[RT], l_sum[RT];  // the row's reference (the same in every wave), and the sum over this lane's tokens
+    f32x4 acc[RT];  // channels 16 wave + 4 lg + e of row lr
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       const int r = rt * 16 + lr;
-      limit[rt] = wstart + (r < rows ? r / a.group_size : T - 1);
-      m_ref[rt] = -INFINITY;
-      accl[rt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int dt = 0; dt < NDT; ++dt) acc[rt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+      limit[rt] = wstart + (r < rows ? div22(r, a.group_size) : T - 1);
+      m_ref[rt] = kNoRef;
+      l_sum[rt] = 0.f;
+      acc[rt] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
+    // Place of chunk c (8 channels) of token j of the V tile: the transpose loads of 16 tokens x 32 bytes, and the
+    // stores of 16 tokens x 16 bytes, spread over all banks.
+    auto v_at = [&](int j, int c) { return sm_v + j * 256 + 16 * (c ^ (((j & 7) << 1) | ((j >> 3) & 1))); };
+    const uint32_t raw_lane = lds_addr(raw) + 16 * lane, raw_scale = lds_addr(raw) + kTpw * 128 + 4 * lr + lg;
+    // this wave's probabilities in sm_p: operand bytes of its 32 tokens (or half of them)
+    char* const p_own = sm_p + (NT == 2 ? wave : wave / 2) * 1024 + lane * 16 + (NT == 2 ? 0 : 8 * (wave & 1));
+    constexpr int kPTile = kTok / 32 * 1024;  // bytes of a row tile
 
-    // A step's rows pass three stages, each a load: its positions, their pages, the rows.
-    struct Pos {
-      int v[2];  // positions of tokens lr and 16 + lr
-    };
-    struct Page {
-      int pos[2], page[2];
-    };
-    struct Rows {
-      u32x4 k[2], v[2];
-      uint32_t ks[2], vs[2];
-    };
-    auto load_pos = [&](int st) {
-      Pos r;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int v = min(st * kStep4 + 16 * i + lr, total - 1);
-        r.v[i] = v < wstart ? (kSparse ? idx_row[v] : v) : N + (v - wstart);
-      }
-      return r;
-    };
-    auto load_page = [&](const Pos& p) {
-      Page r;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        r.pos[i] = clampi(p.v[i], 0, cap_m1);
-        if constexpr (kPaged) r.page[i] = a.k.page_table[(int64_t)b * a.k.max_pages + (r.pos[i] >> a.k.page_shift)];
-        else r.page[i] = b;
-      }
-      return r;
-    };
-    auto load_rows = [&](const Page& p) {
-      Rows r;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        int64_t at = p.page[i], slot = p.pos[i];
-        if constexpr (kPaged) {
-          at = clampi(p.page[i], 0, a.k.num_pages - 1);
-          slot = p.pos[i] & ((1 << a.k.page_shift) - 1);
-        }
-        const int64_t ko = at * (kPaged ? a.k.stride_page : a.k.stride_b) + slot * a.k.stride_n;
-        const int64_t vo = at * (kPaged ? a.v.stride_page : a.v.stride_b) + slot * a.v.stride_n;
-        const int64_t kso = at * (kPaged ? a.k.sstride_page : a.k.sstride_b) + slot * a.k.sstride_n;
-        const int64_t vso = at * (kPaged ? a.v.sstride_page : a.v.sstride_b) + slot * a.v.sstride_n;
-        r.k[i] = *reinterpret_cast<const u32x4*>(kdata + ko);
-        r.v[i] = *reinterpret_cast<const u32x4*>(vdata + vo);
-        r.ks[i] = kscale[kso];
-        r.vs[i] = vscale[vso];
-      }
-      return r;
-    };
-    // LDS place of chunk c (8 channels) of token j of a V tile: the transpose loads of 16 tokens x 32 bytes, and the
-    // stores of 16 tokens x 16 bytes, spread over all banks
-    auto v_at = [&](int j, int c) { return vtile + j * 256 + 16 * (c ^ (((j & 7) << 1) | ((j >> 3) & 1))); };
+    const int rounds = (t_end - t_begin + kTok - 1) / kTok;
+    int slot_n = 0;
+    for (int n = 0; n < rounds; ++n) {
+      if constexpr (!kQReg) asm volatile("" ::: "memory");  // the queries stay in LDS
+      // this round's rows, and the positions and pages that the loads below read
+      wait_loads<(kSlots - 1) * kRawLoads + kExtra>();
+      u32x4 kd[NT], vd[NT];
+      uint32_t kse[NT], vse[NT];
+      if constexpr (NT == 2)
+        asm volatile(
+            "ds_read_b128 %0, %8\n\tds_read_b128 %1, %8 offset:1024\n\tds_read_b128 %2, %8 offset:2048\n\t"
+            "ds_read_b128 %3, %8 offset:3072\n\tds_read_u8 %4, %9\n\tds_read_u8 %5, %9 offset:64\n\t"
+            "ds_read_u8 %6, %9 offset:128\n\tds_read_u8 %7, %9 offset:192\n\ts_waitcnt lgkmcnt(0)"
+            : "=&v"(kd[0]), "=&v"(kd[NT - 1]), "=&v"(vd[0]), "=&v"(vd[NT - 1]), "=&v"(kse[0]), "=&v"(kse[NT - 1]),
+              "=&v"(vse[0]), "=&v"(vse[NT - 1])
+            : "v"(raw_lane + slot_n * kRaw), "v"(raw_scale + slot_n * kRaw)
+            : "memory");
+      else
+        asm volatile(
+            "ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:1024\n\tds_read_u8 %2, %5\n\t"
+            "ds_read_u8 %3, %5 offset:64\n\ts_waitcnt lgkmcnt(0)"
+            : "=&v"(kd[0]), "=&v"(vd[0]), "=&v"(kse[0]), "=&v"(vse[0])
+            : "v"(raw_lane + slot_n * kRaw), "v"(raw_scale + slot_n * kRaw)
+            : "memory");
+      load_pos(n + kSlots + 4);
+      load_page(n + kSlots + 2);
+      load_rows(n + kSlots, slot_n);
+      slot_n = slot_n + 1 == kSlots ? 0 : slot_n + 1;
 
-    auto compute = [&](int st, const Rows& r) {
-      bf16x8 kop[2][4];
+      // ---- scores: lane holds tokens 16 i + 4 lg + e of row lr
+      bf16x8 kop[NT][4];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float ks = kv4_scale(r.ks[i]), vs = kv4_scale(r.vs[i]);
+      for (int i = 0; i < NT; ++i)
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          kop[i][w] = as_bf16x8(kv4_decode8(r.k[i][w], ks));
-          *reinterpret_cast<u32x4*>(v_at(16 * i + lr, 4 * lg + w)) = kv4_decode8(r.v[i][w], vs);
-        }
-      }
-      const int v0 = st * kStep4;
-      const bool edge = v0 + kStep4 - 1 >= wstart;  // wave-uniform: masking only near the window
-      bf16x8 p_op[RT];
+        for (int w = 0; w < 4; ++w) kop[i][w] = as_bf16x8(kv4_decode8(kd[i][w], kv4_scale(kse[i])));
+      f32x4 sc[RT][NT];
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        f32x4 sc[2];
+      for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < NT; ++i) {
           f32x4 c = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int ks = 0; ks < 4; ++ks) {
             if constexpr (kQReg) c = mfma16x16x32(kop[i][ks], qreg[rt][ks], c);
             else c = mfma16x16x32(kop[i][ks], read_q(rt, ks), c);
           }
-          sc[i] = c;
+          sc[rt][i] = c;
         }
-        if (edge)
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (v0 + 16 * i + 4 * lg + e > min(limit[rt], total - 1)) sc[i][e] = -INFINITY;
-        const float m = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
-                              fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
-        const float mx = max_over_lane_groups(m) * a.scale_log2;
-        if (__any(mx > m_ref[rt] + kRescale4)) {
-          const float mn = fmaxf(m_ref[rt], mx);
-          const float alpha = m_ref[rt] == -INFINITY ? 0.f : fast_exp2(m_ref[rt] - mn);
-          m_ref[rt] = mn;
-          accl[rt] *= alpha;
-#pragma unroll
-          for (int dt = 0; dt < NDT; ++dt) acc[rt][dt] *= alpha;
-        }
-        const float nmu = m_ref[rt] == -INFINITY ? 0.f : -m_ref[rt];
-        float p[2][4];
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) p[i][e] = fast_exp2(fmaf(sc[i][e], a.scale_log2, nmu));
-        p_op[rt] = as_bf16x8(u32x4{pk_bf16(p[0][0], p[0][1]), pk_bf16(p[0][2], p[0][3]), pk_bf16(p[1][0], p[1][1]),
-                                   pk_bf16(p[1][2], p[1][3])});
-        const bf16x8 ones = as_bf16x8(u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
-        accl[rt] = mfma16x16x32(ones, p_op[rt], accl[rt]);
-      }
-      // V^T of 16 channels over the step's tokens: token 4 lg + e, and 16 + 4 lg + e
-      const int j0 = 4 * lg + (lr >> 2);
-#pragma unroll
-      for (int dt = 0; dt < NDT; ++dt) {
-        const int c = 2 * dt + ((lr >> 1) & 1);
-        const u32x2 lo = read_tr16(v_at(j0, c) + 8 * (lr & 1)), hi = read_tr16(v_at(j0 + 16, c) + 8 * (lr & 1));
-        const bf16x8 vt = as_bf16x8(u32x4{lo[0], lo[1], hi[0], hi[1]});
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) acc[rt][dt] = mfma16x16x32(vt, p_op[rt], acc[rt][dt]);
-      }
-    };
-
-    const int st0 = s_begin + wave;
-    Pos pos = load_pos(st0);
-    Page page = load_page(pos);
-    pos = load_pos(st0 + 4);
-    Rows ra = load_rows(page);
-    page = load_page(pos);
-    pos = load_pos(st0 + 8);
-    Rows rb = load_rows(page);
-    page = load_page(pos);
-    pos = load_pos(st0 + 12);
-    for (int st = st0; st < s_end; st += 8) {
-      compute(st, ra);
-      {
-        const Page now = page;
-        page = load_page(pos);
-        pos = load_pos(st + 16);
-        ra = load_rows(now);
-      }
-      if (st + 4 >= s_end) break;
-      compute(st + 4, rb);
-      {
-        const Page now = page;
-        page = load_page(pos);
-        pos = load_pos(st + 20);
-        rb = load_rows(now);
-      }
-    }
-
-    // the waves' parts become one: each at the rows' largest reference, summed in a fixed order
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
-      if (lg == 0) {
-        sm_m[wave][rt * 16 + lr] = m_ref[rt];
-        sm_l[wave][rt * 16 + lr] = accl[rt][0];
-      }
-    __syncthreads();  // (and the V tiles are free)
-    float* const buf = reinterpret_cast<float*>(smem);
-    float beta[RT];
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      const int r = rt * 16 + lr;
-      const float M = fmaxf(fmaxf(sm_m[0][r], sm_m[1][r]), fmaxf(sm_m[2][r], sm_m[3][r]));
-      beta[rt] = m_ref[rt] == -INFINITY ? 0.f : fast_exp2(m_ref[rt] - M);
-    }
-    for (int round = 0; round < kW4 / kNB; ++round) {
-      if (wave / kNB == round)
+      const int v0 = t_begin + n * kTok + wave * kTpw;
+      if (v0 + kTpw - 1 >= min(wstart, t_end))  // wave-uniform: masking only near the window and the end
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-          for (int dt = 0; dt < NDT; ++dt) {
-            f32x4* at = reinterpret_cast<f32x4*>(buf + (wave % kNB) * kBuf + (rt * 16 + lr) * kPitch + 16 * dt + 4 * lg);
-            const f32x4 x = acc[rt][dt] * beta[rt];
-            *at = round ? *at + x : x;
-          }
-      __syncthreads();
-    }
-    const bool whole = g0 == pair_g && g1 == pair_end;
-    const int64_t slot = (2 * unit + (g0 != start ? 1 : 0)) * a.rows_max;
-    for (int e = threadIdx.x; e < rows * (kD4 / 8); e += kW4 * kWave) {
-      const int r = e / (kD4 / 8), c0 = (e % (kD4 / 8)) * 8;
-      float M = -INFINITY, L = 0.f;
+          for (int i = 0; i < NT; ++i)
 #pragma unroll
-      for (int w = 0; w < kW4; ++w) M = fmaxf(M, sm_m[w][r]);
+            for (int e = 0; e < 4; ++e)
+              if (v0 + 16 * i + 4 * lg + e > min(limit[rt], t_end - 1)) sc[rt][i][e] = -INFINITY;
+
+      // ---- probabilities
+      u32x2 p_op[RT][NT];
+      float p_sum[RT];
+      auto probabilities = [&](int rt) {
+        float s[NT];
 #pragma unroll
-      for (int w = 0; w < kW4; ++w) L += sm_m[w][r] == -INFINITY ? 0.f : sm_l[w][r] * fast_exp2(sm_m[w][r] - M);
-      const float* x = buf + r * kPitch + c0;
-      f32x4 lo = *reinterpret_cast<const f32x4*>(x), hi = *reinterpret_cast<const f32x4*>(x + 4);
-      if constexpr (kNB == 2) {
-        lo += *reinterpret_cast<const f32x4*>(x + kBuf);
-        hi += *reinterpret_cast<const f32x4*>(x + kBuf + 4);
+        for (int i = 0; i < NT; ++i) {
+          float p[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) p[e] = fast_exp2(fmaf(sc[rt][i][e], a.scale_log2, -m_ref[rt]));
+          p_op[rt][i] = u32x2{pk_bf16(p[0], p[1]), pk_bf16(p[2], p[3])};
+          s[i] = (p[0] + p[1]) + (p[2] + p[3]);
+        }
+        p_sum[rt] = NT == 2 ? s[0] + s[NT - 1] : s[0];
+      };
+      auto own_max = [&](int rt) {
+        float m = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+          m = fmaxf(m, fmaxf(fmaxf(sc[rt][i][0], sc[rt][i][1]), fmaxf(sc[rt][i][2], sc[rt][i][3])));
+        return m * a.scale_log2;
+      };
+      bool over = false;
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        probabilities(rt);
+        over |= own_max(rt) > m_ref[rt] + kRescale4;
       }
+      auto write_p = [&]() {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          if constexpr (NT == 2)
+            *reinterpret_cast<u32x4*>(p_own + rt * kPTile) =
+                u32x4{p_op[rt][0][0], p_op[rt][0][1], p_op[rt][NT - 1][0], p_op[rt][NT - 1][1]};
+          else *reinterpret_cast<u32x2*>(p_own + rt * kPTile) = p_op[rt][0];
+        }
+      };
+      lds_barrier4();  // the waves are done with the round before
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+          *reinterpret_cast<u32x4*>(v_at(wave * kTpw + 16 * i + lr, 4 * lg + w)) =
+              kv4_decode8(vd[i][w], kv4_scale(vse[i]));
+      write_p();
+      const int any_over = __any(over) ? 1 : 0;
+      if (lane == 0) sm_over[n & 1][wave] = any_over;
+      lds_barrier4();
+      const u32x4 o0 = *reinterpret_cast<const u32x4*>(&sm_over[n & 1][0]);
+      const u32x4 o1 = *reinterpret_cast<const u32x4*>(&sm_over[n & 1][4]);
+      const uint32_t moves = (o0[0] | o0[1] | o0[2] | o0[3]) | (o1[0] | o1[1] | o1[2] | o1[3]);
+      if (__builtin_amdgcn_readfirstlane(moves)) {
+        // a row's maximum is far above its reference (in the first round, and seldom after): all references move
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          const float m = max_over_lane_groups(own_max(rt));
+          if (lg == 0) sm_max[wave][rt * 16 + lr] = m;
+        }
+        lds_barrier4();
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          float mn = m_ref[rt];
+#pragma unroll
+          for (int w = 0; w < kW4; ++w) mn = fmaxf(mn, sm_max[w][rt * 16 + lr]);
+          const float alpha = fast_exp2(m_ref[rt] - mn);
+          m_ref[rt] = mn;
+          l_sum[rt] *= alpha;
+          acc[rt] *= alpha;
+          probabilities(rt);
+        }
+        write_p();
+        lds_barrier4();
+      }
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) l_sum[rt] += p_sum[rt];
+
+      // ---- O^T of 16 channels: token 32 k + 4 lg + e, and 32 k + 16 + 4 lg + e
+      const int left = t_end - (t_begin + n * kTok);
+      const int j0 = 4 * lg + (lr >> 2), c = 2 * wave + ((lr >> 1) & 1);
+#pragma unroll
+      for (int k = 0; k < kTok / 32; ++k) {
+        if (k > 0 && 32 * k >= left) break;
+        const u32x2 lo = read_tr16(v_at(32 * k + j0, c) + 8 * (lr & 1));
+        const u32x2 hi = read_tr16(v_at(32 * k + j0 + 16, c) + 8 * (lr & 1));
+        const bf16x8 vt = as_bf16x8(u32x4{lo[0], lo[1], hi[0], hi[1]});
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+          acc[rt] = mfma16x16x32(
+              vt, as_bf16x8(*reinterpret_cast<const u32x4*>(sm_p + rt * kPTile + k * 1024 + lane * 16)), acc[rt]);
+      }
+    }
+    wait_loads<0>();
+
+    // ---- the rows' sums over all waves, and the outputs
+    lds_barrier4();
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const float l = sum_over_lane_groups(l_sum[rt]);
+      if (lg == 0) sm_max[wave][rt * 16 + lr] = l;
+    }
+    lds_barrier4();
+    const bool whole = g0 == pair_g && g1 == pair_end;
+    const int64_t part = ((int64_t)2 * unit + (g0 != start ? 1 : 0)) * a.rows_max;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const int r = rt * 16 + lr;
+      float L = 0.f;
+#pragma unroll
+      for (int w = 0; w < kW4; ++w) L += sm_max[w][r];
+      if (r >= rows) continue;
       if (whole) {
-        const float inv = 1.f / L;
-        lo *= inv;
-        hi *= inv;
-        const int t = r / a.group_size, hh = r - t * a.group_size;
-        *reinterpret_cast<u32x4*>(a.out + b * a.o_sb + t * a.o_st + (g * a.group_size + hh) * a.o_sh + c0) =
-            u32x4{pk_bf16(lo[0], lo[1]), pk_bf16(lo[2], lo[3]), pk_bf16(hi[0], hi[1]), pk_bf16(hi[2], hi[3])};
+        const f32x4 x = acc[rt] * (1.f / L);
+        const int t = div22(r, a.group_size), hh = r - t * a.group_size;
+        *reinterpret_cast<u32x2*>(a.out + b * a.o_sb + t * a.o_st + (g * a.group_size + hh) * a.o_sh + 16 * wave +
+                                  4 * lg) = u32x2{pk_bf16(x[0], x[1]), pk_bf16(x[2], x[3])};
       } else {
-        float* p = a.part + (slot + r) * kD4 + c0;
-        *reinterpret_cast<f32x4*>(p) = lo;
-        *reinterpret_cast<f32x4*>(p + 4) = hi;
-        if (c0 == 0) a.part_ml[slot + r] = make_float2(M, L);
+        *reinterpret_cast<f32x4*>(a.part + (part + r) * kD4 + 16 * wave + 4 * lg) = acc[rt];
+        if (wave == 0 && lg == 0) a.part_ml[part + r] = make_float2(m_ref[rt], L);
       }
     }
     g0 = g1;
@@ -388,68 +510,70 @@ __global__ __launch_bounds__(kW4 * kWave) void attn_kv4_kernel(Attn4Args a) {
   }
 }
 
-// Joins the parts of pair blockIdx.x: 16 threads to a row, eight channels each, the parts in order.
+// Joins the parts of a pair: a workgroup for a query row, eight parts at a time, four channels to a thread; the eight
+// sums are added in order.
 template <bool kSparse>
-__global__ __launch_bounds__(kW4 * kWave) void attn_kv4_merge_kernel(Attn4Args a) {
-  __shared__ int64_t sm_scan[kW4];
-  __shared__ int64_t sm_first;
-  const int pair = blockIdx.x;
-  int64_t total_g, before;
-  int p0, p1;
-  scan_pairs(a, kSparse, sm_scan, p0, p1, before, total_g);
-  if (p0 <= pair && pair < p1) {
-    for (int p = p0; p < pair; ++p) before += granules_of(a, kSparse, p);
-    sm_first = before;
-  }
-  __syncthreads();
-  const int64_t per = run_length(a, total_g), first = sm_first;
-  const int n_g = granules_of(a, kSparse, pair);
-  if (n_g == 0) return;
-  const int64_t u0 = first / per, u1 = (first + n_g - 1) / per;
+__global__ __launch_bounds__(256) void attn_kv4_merge_kernel(Attn4Args a) {
+  __shared__ f32x4 sm_acc[8][32];
+  __shared__ float sm_l[8];
+  const int pair = blockIdx.x, r = blockIdx.y;
+  const int b = div22(pair, a.num_kv_heads), g = pair - b * a.num_kv_heads;
+  const Pair4 pr = pair_of<kSparse>(a, pair);
+  const int per = a.plan[0], first = a.plan[1 + pair];
+  const int n_g = pr.granules();
+  if (n_g == 0 || r >= pr.T * a.group_size) return;
+  const int u0 = first / per, u1 = (first + n_g - 1) / per;
   if (u0 == u1) return;
-  const int b = pair / a.num_kv_heads, g = pair - b * a.num_kv_heads;
-  const int rows = a.dims.nq(b) * a.group_size;
-  const int r = (blockIdx.y * kW4 * kWave + threadIdx.x) / 16, c0 = (threadIdx.x % 16) * 8;
-  if (r >= rows) return;
-  auto slot_of = [&](int64_t u) { return (2 * u + (u == u0 && u0 * per < first ? 1 : 0)) * a.rows_max + r; };
-  float M = -INFINITY;
-  for (int64_t u = u0; u <= u1; ++u) M = fmaxf(M, a.part_ml[slot_of(u)].x);
-  f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
+  const int part = threadIdx.x / 32, c0 = (threadIdx.x % 32) * 4;
+  auto slot_of = [&](int u) { return ((int64_t)2 * u + (u == u0 && u0 * per < first ? 1 : 0)) * a.rows_max + r; };
+  float M = kNoRef;
+  for (int u = u0 + (threadIdx.x & 31); u <= u1; u += 32) M = fmaxf(M, a.part_ml[slot_of(u)].x);
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) M = fmaxf(M, __shfl_xor(M, d));
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
   float L = 0.f;
-  for (int64_t u = u0; u <= u1; ++u) {
+  for (int u = u0 + part; u <= u1; u += 8) {
     const int64_t s = slot_of(u);
     const float2 ml = a.part_ml[s];
-    const float w = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - M);
+    const float w = fast_exp2(ml.x - M);
     L += w * ml.y;
-    lo += w * *reinterpret_cast<const f32x4*>(a.part + s * kD4 + c0);
-    hi += w * *reinterpret_cast<const f32x4*>(a.part + s * kD4 + c0 + 4);
+    x += w * *reinterpret_cast<const f32x4*>(a.part + s * kD4 + c0);
   }
-  const float inv = 1.f / L;
-  lo *= inv;
-  hi *= inv;
-  const int t = r / a.group_size, hh = r - t * a.group_size;
-  *reinterpret_cast<u32x4*>(a.out + b * a.o_sb + t * a.o_st + (g * a.group_size + hh) * a.o_sh + c0) =
-      u32x4{pk_bf16(lo[0], lo[1]), pk_bf16(lo[2], lo[3]), pk_bf16(hi[0], hi[1]), pk_bf16(hi[2], hi[3])};
+  sm_acc[part][threadIdx.x % 32] = x;
+  if (c0 == 0) sm_l[part] = L;
+  __syncthreads();
+  if (threadIdx.x >= 32) return;
+  L = sm_l[0];
+  for (int i = 1; i < 8; ++i) {
+    x += sm_acc[i][threadIdx.x];
+    L += sm_l[i];
+  }
+  x *= 1.f / L;
+  const int t = div22(r, a.group_size), hh = r - t * a.group_size;
+  *reinterpret_cast<u32x2*>(a.out + b * a.o_sb + t * a.o_st + (g * a.group_size + hh) * a.o_sh + c0) =
+      u32x2{pk_bf16(x[0], x[1]), pk_bf16(x[2], x[3])};
 }
 
 template <bool kSparse, bool kPaged>
 hipError_t launch_rt(const Attn4Args& a, int rt, hipStream_t stream) {
-  const dim3 grid((unsigned)a.units), block(kW4 * kWave);
   switch (rt) {
-#define CASE(n) \
-  case n: hipLaunchKernelGGL((attn_kv4_kernel<n, kSparse, kPaged>), grid, block, 0, stream, a); break;
+#define CASE(n)                                                                                                  \
+  case n:                                                                                                        \
+    hipLaunchKernelGGL((attn_kv4_kernel<n, kSparse, kPaged>), dim3((unsigned)a.units), dim3(kThreads4), 0, stream, a); \
+    break;
     CASE(1) CASE(2) CASE(3) CASE(4) CASE(5) CASE(6) CASE(8)
 #undef CASE
     default: return hipErrorInvalidValue;
   }
-  hipLaunchKernelGGL((attn_kv4_merge_kernel<kSparse>), dim3((unsigned)a.pairs, (unsigned)((a.rows_max + 15) / 16)),
-                     block, 0, stream, a);
+  hipLaunchKernelGGL((attn_kv4_merge_kernel<kSparse>), dim3((unsigned)a.pairs, (unsigned)a.rows_max), dim3(256), 0,
+                     stream, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_attn_kv4(const Attn4Args& a, int rt, bool sparse, bool paged, hipStream_t stream) {
+  if (rt == 7) rt = 8;
   if (sparse) return paged ? launch_rt<true, true>(a, rt, stream) : launch_rt<true, false>(a, rt, stream);
   return paged ? launch_rt<false, true>(a, rt, stream) : launch_rt<false, false>(a, rt, stream);
 }

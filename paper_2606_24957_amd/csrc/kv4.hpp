@@ -96,7 +96,7 @@ struct EvictArgs {
 hipError_t launch_evict(const EvictArgs& a, hipStream_t stream);
 
 // ---- verification attention over a 4-bit cache (attn_kv4.hip) ----
-constexpr int kAttn4Granule = 128;  // tokens: one 32-token step for each of a workgroup's four waves
+constexpr int kAttn4Granule = 128;  // tokens
 
 struct Attn4Args {
   const uint16_t* q;
@@ -111,11 +111,13 @@ struct Attn4Args {
   int32_t groups;
   int32_t num_kv_heads, group_size, pairs;
   float scale_log2;
-  int32_t units;         // workgroups, a multiple of 8
+  int32_t idx_last;      // last entry of a selection's row
+  int32_t units;         // runs at most, a multiple of 8
   int32_t min_granules;  // smallest run of a workgroup
   int32_t rows_max;      // query rows of a KV head, at most
   float* part;           // [units][2][rows_max][128]
   float2* part_ml;       // [units][2][rows_max]
+  int32_t* plan;         // a run's length, then each pair's first granule
 };
 hipError_t launch_attn_kv4(const Attn4Args& a, int rt, bool sparse, bool paged, hipStream_t stream);
 

@@ -585,6 +585,65 @@ dustin_status dustin_kv4_evict(const dustin_kv4* k, const dustin_kv4* v, const d
                                int32_t* new_lens, void* stream);
 
 /* ---------------------------------------------------------------------------------
+ * dustin_sample -- next tokens from logits, with temperature, top-k, top-p and min-p, from given random numbers.
+ * For every sequence b, with top the largest logit and w_i = exp((l_i - top) / temperature) (1 where l_i = top; a
+ * weight below 2^-45 counts as zero, and so does that of a logit that is -infinity or NaN):
+ *   the kept set is, in the order of (logit descending, index ascending), the top_k first; of those the fewest whose
+ *   weights add up to at least top_p of theirs; of those the ones with w_i >= min_p.  The first is always kept.
+ *   token[b] = the smallest i at which the running sum of the kept weights, by index, passes u[b] of the whole
+ *   probs[b, i] = w_i over the sum of the kept weights, 0 outside the kept set
+ * temperature <= 0 keeps the first alone (the largest logit, of equal ones the lowest index); top_k <= 0 or >= vocab,
+ * top_p >= 1 and min_p <= 0 keep all; min_p > 1 counts as 1.  u is clamped to [0, 1).  A row without a logit above
+ * -infinity (all masked) gives token -1 and probabilities 0.
+ *   logits     bf16 or fp32 [batch, vocab] (dtype; stride l_sb in elements, rows contiguous, of any alignment)
+ *   vocab      1 ... 2^18;  batch <= 65535
+ *   set        the settings: a device array [batch] where one is given, else the scalar for every sequence
+ *   u          fp32 [batch];  token  int32 [batch]
+ *   probs      fp32 [batch, vocab] (stride probs_sb) or NULL
+ *   workspace  dustin_sample_workspace(batch, 1, vocab, dtype) bytes, 256-byte aligned.  Its first 256 KB must be zero
+ *              before the first call; every call leaves them zero, so one buffer can serve calls of any shape.  Calls
+ *              that share a workspace must not overlap.
+ * Weights are computed in fp64 and summed as multiples of 2^-44: results do not depend on the order of the sums.
+ *
+ * dustin_verify_sample -- the drafted tokens of a verification window against the target's logits (speculative
+ * sampling): the output is distributed as the target's own samples would be.  For every sequence b with T = T_b
+ * window tokens (the last accepted token and T - 1 drafts), p_t the distribution that dustin_sample would draw from at
+ * row t, x_t = draft[b, t] and q_t = draft_probs[b, t] (NULL: the drafts were certain, q_t(x_t) = 1):
+ *   draft t is accepted if all before it are and u_accept[b, t] q_t(x_t) < p_t(x_t)
+ *   accepted[b] = 1 + the number of accepted drafts: the window tokens to keep, as dustin_kv_commit takes them
+ *   token[b]    = drawn with u[b] as above from max(p_t - q_t, 0) of the first rejected draft t (from p_t where that is
+ *                 zero everywhere), or from p_{T-1} where every draft is accepted
+ * T = 0 gives accepted 0 and token -1.  A draft outside [0, vocab) is rejected.
+ *   logits     [batch, nq_max, vocab] (strides l_sb, l_st); row t follows window token t;  1 <= nq_max <= 64
+ *   n_query    int32 [batch] (T_b) or NULL (= nq_max)
+ *   draft, u_accept  int32, fp32 [batch, >= nq_max - 1] (strides draft_sb, ua_sb)
+ *   draft_probs      fp32 [batch, >= nq_max - 1, vocab] (strides q_sb, q_st), as dustin_sample's probs
+ *   accepted, token  int32 [batch]
+ *   workspace  dustin_sample_workspace(batch, nq_max, vocab, dtype) bytes, as above;  batch * nq_max <= 65535
+ * --------------------------------------------------------------------------------- */
+#define DUSTIN_BF16 0
+#define DUSTIN_F32 1
+typedef struct {
+  float temperature;
+  int32_t top_k;
+  float top_p, min_p;
+  const float* temperature_b; /* device arrays [batch] or NULL */
+  const int32_t* top_k_b;
+  const float* top_p_b;
+  const float* min_p_b;
+} dustin_sampling;
+size_t dustin_sample_workspace(int32_t batch, int32_t nq_max, int32_t vocab, int32_t dtype);
+dustin_status dustin_sample(const void* logits, int32_t dtype, int64_t l_sb, int32_t batch, int32_t vocab,
+                            const dustin_sampling* set, const float* u, int32_t* token, float* probs, int64_t probs_sb,
+                            void* workspace, size_t workspace_bytes, void* stream);
+dustin_status dustin_verify_sample(const void* logits, int32_t dtype, int64_t l_sb, int64_t l_st, int32_t batch,
+                                   int32_t nq_max, const int32_t* n_query, int32_t vocab, const dustin_sampling* set,
+                                   const int32_t* draft, int64_t draft_sb, const float* draft_probs, int64_t q_sb,
+                                   int64_t q_st, const float* u_accept, int64_t ua_sb, const float* u,
+                                   int32_t* accepted, int32_t* token, void* workspace, size_t workspace_bytes,
+                                   void* stream);
+
+/* ---------------------------------------------------------------------------------
  * dustin_read_probe -- a plain streaming read of a device buffer, for measurement only (no
  * part of the method): the practical read rate of the GPU, against which the rates of the
  * bandwidth-bound kernels above are reported.  Workgroup g of `blocks` reads the g-th of

@@ -33,7 +33,7 @@ EXPORTED = ("dustin_status_string", "dustin_version", "dustin_score_workspace", 
             "dustin_sparse_verify_attn_noalloc", "dustin_score_calls", "dustin_read_probe",
             "dustin_kv4_append", "dustin_kv4_read", "dustin_attn_kv4_workspace",
             "dustin_sparse_verify_attn_kv4", "dustin_dense_verify_attn_kv4", "dustin_kv_evict",
-            "dustin_kv4_evict")
+            "dustin_kv4_evict", "dustin_sample_workspace", "dustin_sample", "dustin_verify_sample")
 
 
 class DustinError(RuntimeError):
@@ -59,6 +59,12 @@ class DustinKV4(ctypes.Structure):
                 ("capacity", ctypes.c_int64), ("page_table", ctypes.c_void_p), ("page_size", ctypes.c_int32),
                 ("max_pages", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("stride_page", ctypes.c_int64),
                 ("scale_stride_page", ctypes.c_int64)]
+
+
+class DustinSampling(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_float), ("top_k", ctypes.c_int32), ("top_p", ctypes.c_float),
+                ("min_p", ctypes.c_float), ("temperature_b", ctypes.c_void_p), ("top_k_b", ctypes.c_void_p),
+                ("top_p_b", ctypes.c_void_p), ("min_p_b", ctypes.c_void_p)]
 
 
 class DustinBatch(ctypes.Structure):
@@ -165,6 +171,14 @@ def lib():
             f.restype = ctypes.c_int
             f.argtypes = [P, P, P, P, _i32, _vp, _i64, _i64, _vp, _i32, _i32, _vp, _i64, _i64, _i32, _vp, _i64, _i64,
                           _vp, _vp]
+        P_SET = ctypes.POINTER(DustinSampling)
+        L.dustin_sample_workspace.restype = _sz
+        L.dustin_sample_workspace.argtypes = [_i32, _i32, _i32, _i32]
+        L.dustin_sample.restype = ctypes.c_int
+        L.dustin_sample.argtypes = [_vp, _i32, _i64, _i32, _i32, P_SET, _vp, _vp, _vp, _i64, _vp, _sz, _vp]
+        L.dustin_verify_sample.restype = ctypes.c_int
+        L.dustin_verify_sample.argtypes = [_vp, _i32, _i64, _i64, _i32, _i32, _vp, _i32, P_SET, _vp, _i64, _vp, _i64, _i64,
+                                           _vp, _i64, _vp, _vp, _vp, _vp, _sz, _vp]
         _lib = L
     return _lib
 
@@ -1082,3 +1096,106 @@ def plan_kv_evict(k, v, idx: torch.Tensor, count: torch.Tensor, *, k_out=None, v
 def kv_evict(k, v, idx, count, **kw):
     """The kept rows of a layer's caches to the front of others (or in place); returns (k_out, v_out)."""
     return plan_kv_evict(k, v, idx, count, **kw)()
+
+
+# ----------------------------------------------------------------------------- sampling and verification of drafts
+
+_LOGITS = {torch.bfloat16: 0, torch.float32: 1}
+
+
+def _sampling(temperature, top_k, top_p, min_p, B, dev) -> DustinSampling:
+    """The settings: numbers for every sequence, or tensors [B] of one for each."""
+    s = DustinSampling(1.0, 0, 1.0, 0.0, None, None, None, None)
+    keep = []
+    for name, x, dt in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
+                        ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
+        if isinstance(x, torch.Tensor):
+            _on_gpu(x)
+            if x.dtype != dt or x.shape != (B,):
+                raise ValueError(f"{name} must be a number or a {dt} tensor [{B}]")
+            x = x.contiguous()
+            keep.append(x)
+            setattr(s, name + "_b", x.data_ptr())
+        else:
+            setattr(s, name, x)
+    s._keep = keep
+    return s
+
+
+def _vector(x, B, dt, name):
+    if x.dtype != dt or x.shape != (B,) or not x.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dt} tensor [{B}]")
+
+
+def plan_sample(logits: torch.Tensor, u: torch.Tensor, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
+                token: Optional[torch.Tensor] = None, probs: Optional[torch.Tensor] = None, stream=None) -> Call:
+    """Prepared dustin_sample: next tokens int32 [B] from logits bf16 or fp32 [B, V] and random numbers u fp32 [B] in
+    [0, 1).  The settings are numbers or tensors [B].  With probs (fp32 [B, V]) the call also writes the distributions
+    that the tokens are drawn from, and returns (token, probs)."""
+    _on_gpu(logits, u, token, probs)
+    if logits.dtype not in _LOGITS or logits.dim() != 2 or (logits.stride(1) != 1 and logits.shape[1] > 1):
+        raise ValueError("logits must be bf16 or fp32 [B, V] with contiguous rows")
+    B, V = logits.shape
+    dev, dtype = logits.device, _LOGITS[logits.dtype]
+    _vector(u, B, torch.float32, "u")
+    if token is None:
+        token = torch.empty(B, dtype=torch.int32, device=dev)
+    _vector(token, B, torch.int32, "token")
+    if probs is not None and (probs.dtype != torch.float32 or probs.shape != logits.shape or
+                              (probs.stride(1) != 1 and V > 1)):
+        raise ValueError("probs must be fp32 of the logits' shape with contiguous rows")
+    s = _sampling(temperature, top_k, top_p, min_p, B, dev)
+    nbytes = lib().dustin_sample_workspace(B, 1, V, dtype)
+    ws = workspace(nbytes, dev, "sample", stream)
+    args = (_ptr(logits), dtype, logits.stride(0), B, V, ctypes.byref(s), _ptr(u), _ptr(token), _ptr(probs),
+            0 if probs is None else probs.stride(0), _ptr(ws), nbytes, _stream(stream))
+    return Call(lib().dustin_sample, args, "dustin_sample", (logits, u, s, ws),
+                token if probs is None else (token, probs))
+
+
+def sample(logits, u, **kw):
+    """Next tokens from logits; returns token int32 [B], or (token, probs) where probs is given."""
+    return plan_sample(logits, u, **kw)()
+
+
+def plan_verify_tokens(logits: torch.Tensor, draft: torch.Tensor, u_accept: torch.Tensor, u: torch.Tensor, *,
+                       draft_probs: Optional[torch.Tensor] = None, n_query=None, temperature=1.0, top_k=0, top_p=1.0,
+                       min_p=0.0, accepted: Optional[torch.Tensor] = None, token: Optional[torch.Tensor] = None,
+                       stream=None) -> Call:
+    """Prepared dustin_verify_sample: logits bf16 or fp32 [B, T, V] of the window's tokens, draft int32 [B, T - 1],
+    draft_probs fp32 [B, T - 1, V] (None: greedy drafts), random numbers u_accept fp32 [B, T - 1] and u fp32 [B].
+    Returns (accepted, token) int32 [B]: the window tokens to keep, as kv_commit takes them, and the next token."""
+    _on_gpu(logits, draft, u_accept, u, draft_probs, accepted, token)
+    if logits.dtype not in _LOGITS or logits.dim() != 3 or (logits.stride(2) != 1 and logits.shape[2] > 1):
+        raise ValueError("logits must be bf16 or fp32 [B, T, V] with contiguous rows")
+    B, T, V = logits.shape
+    dev, dtype = logits.device, _LOGITS[logits.dtype]
+    for x, dt, name in ((draft, torch.int32, "draft"), (u_accept, torch.float32, "u_accept")):
+        if x.dtype != dt or x.shape != (B, T - 1) or (T > 2 and x.stride(1) != 1):
+            raise ValueError(f"{name} must be {dt} [{B}, {T - 1}] with contiguous rows")
+    if draft_probs is not None and (draft_probs.dtype != torch.float32 or draft_probs.shape != (B, T - 1, V) or
+                                    (draft_probs.stride(2) != 1 and V > 1)):
+        raise ValueError(f"draft_probs must be fp32 [{B}, {T - 1}, {V}] with contiguous rows")
+    _vector(u, B, torch.float32, "u")
+    accepted = torch.empty(B, dtype=torch.int32, device=dev) if accepted is None else accepted
+    token = torch.empty(B, dtype=torch.int32, device=dev) if token is None else token
+    _vector(accepted, B, torch.int32, "accepted")
+    _vector(token, B, torch.int32, "token")
+    nqa = _i32_dev(n_query, dev)
+    if nqa is not None:
+        _vector(nqa, B, torch.int32, "n_query")
+    s = _sampling(temperature, top_k, top_p, min_p, B, dev)
+    nbytes = lib().dustin_sample_workspace(B, T, V, dtype)
+    ws = workspace(nbytes, dev, "sample", stream)
+    q = draft_probs if T > 1 else None
+    args = (_ptr(logits), dtype, logits.stride(0), logits.stride(1), B, T, _ptr(nqa), V, ctypes.byref(s),
+            _ptr(draft) if T > 1 else None, draft.stride(0), _ptr(q), 0 if q is None else q.stride(0),
+            0 if q is None else q.stride(1), _ptr(u_accept) if T > 1 else None, u_accept.stride(0), _ptr(u),
+            _ptr(accepted), _ptr(token), _ptr(ws), nbytes, _stream(stream))
+    return Call(lib().dustin_verify_sample, args, "dustin_verify_sample",
+                (logits, draft, u_accept, u, draft_probs, nqa, s, ws), (accepted, token))
+
+
+def verify_tokens(logits, draft, u_accept, u, **kw):
+    """Drafted tokens against the target's logits; returns (accepted, token)."""
+    return plan_verify_tokens(logits, draft, u_accept, u, **kw)()

@@ -10,7 +10,7 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libdustin.so")
 SOURCES = ["score_once_pair.hip", "score_once.hip", "api.hip", "attn.hip", "score.hip", "score_sync.hip",
            "score_reread.hip", "topk.hip", "kv.hip", "page.hip", "arr.hip", "probe.hip",
-           "api_kv4.hip", "kv4.hip", "evict.hip", "attn_kv4.hip"]
+           "api_kv4.hip", "kv4.hip", "evict.hip", "attn_kv4.hip", "api_sample.hip", "sample.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 

@@ -1,0 +1,65 @@
+// sample.hpp -- argument blocks of the sampling kernels (internal).
+#pragma once
+
+#include "kernels.hpp"
+
+namespace dustin {
+
+// Tokens are ranked by (logit descending, index ascending) through one number, smaller for the better: the logit's
+// order-preserving key, complemented, over the index.
+constexpr int kSampleIdxBits = 18;
+constexpr int kSampleMaxVocab = 1 << kSampleIdxBits;
+
+// A token's weight, 2^((x - top) log2(e) / T) of the row's largest logit, is summed as a multiple of 2^-44: sums of
+// integers do not depend on their order, 2^18 tokens stay below 2^62, and a weight is off by at most 2^-45.  Weights
+// below 2^-45 count as zero.
+constexpr int kSampleFrac = 44;
+constexpr int kSampleBins = 184;     // quarter octaves from the largest weight down to 2^-45.5, and one
+constexpr int kSampleMaxWindow = 64; // tokens of a verification window
+constexpr int kSampleMaxChunks = 264;  // 2^18 fp32 logits in chunks of 256 pieces, wherever the row begins
+
+struct SampleRow {  // what is known of a row once its filters are resolved
+  uint64_t last;    // rank of the last kept token (0: none is)
+  uint64_t sum;     // of the kept weights
+  float top;        // largest logit
+};
+
+struct SampleArgs {
+  const void* logits;
+  int64_t sb, st;  // strides of sequences and of a sequence's rows, in elements
+  int32_t batch, rows_per_seq, vocab;
+  const int32_t* n_query;  // rows of a sequence, or NULL (= rows_per_seq)
+  const float* temperature;
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;  // [batch] or NULL: the scalars
+  float s_temperature, s_top_p, s_min_p;
+  int32_t s_top_k;
+  const float* u;  // [batch]
+  int32_t* token;  // [batch]
+  float* probs;    // sampling: [batch][vocab] or NULL
+  int64_t probs_sb;
+  // verification
+  const int32_t* draft;
+  int64_t draft_sb;
+  const float* q;  // or NULL: the drafts were certain
+  int64_t q_sb, q_st;
+  const float* u_accept;
+  int64_t ua_sb;
+  int32_t* accepted;
+  // chunks of `granules` 16-byte pieces, `chunks` to a row, and what is kept of them
+  int32_t granules, chunks;
+  float* c_top;       // [rows][chunks] largest logit
+  uint64_t* c_best;   // best rank
+  uint64_t* c_sum;    // sum of weights, against the chunk's largest
+  uint64_t* h_sum;    // [rows][chunks][kSampleBins]
+  uint32_t* h_cnt;
+  SampleRow* row;     // [rows]
+  uint64_t* r_sum;    // [batch][chunks][2]: sums of what is left of the distribution, and of it whole
+  uint32_t* arrived;  // [batch], zero between calls
+};
+
+hipError_t launch_sample(const SampleArgs& a, bool bf16, hipStream_t stream);
+hipError_t launch_verify_sample(const SampleArgs& a, bool bf16, hipStream_t stream);
+
+}  // namespace dustin

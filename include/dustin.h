@@ -600,7 +600,7 @@ dustin_status dustin_kv4_evict(const dustin_kv4* k, const dustin_kv4* v, const d
  *   set        the settings: a device array [batch] where one is given, else the scalar for every sequence
  *   u          fp32 [batch];  token  int32 [batch]
  *   probs      fp32 [batch, vocab] (stride probs_sb) or NULL
- *   workspace  dustin_sample_workspace(batch, 1, vocab, dtype) bytes, 256-byte aligned.  Its first 256 KB must be zero
+ *   workspace  dustin_sample_workspace(batch, 1, vocab, dtype) bytes, 256-byte aligned.  Its first 512 KB must be zero
  *              before the first call; every call leaves them zero, so one buffer can serve calls of any shape.  Calls
  *              that share a workspace must not overlap.
  * Weights are computed in fp64 and summed as multiples of 2^-44: results do not depend on the order of the sums.

@@ -18,10 +18,12 @@ int granules_of(int64_t rows, int64_t pieces) {
   return 256;
 }
 
-// The workspace begins with the arrival counters, whatever a call's sizes are.
+constexpr size_t kCounters = (kMaxRows + 1) * sizeof(uint32_t);  // of each kind
+
+// The workspace begins with the arrival and list counters, whatever a call's sizes are.
 struct SampleWs {
   int granules, chunks;
-  size_t row, c_top, c_best, c_sum, r_sum, h_cnt, h_sum, total;
+  size_t row, plan, list, c_top, c_best, c_sum, r_sum, h_cnt, h_sum, total;
 };
 
 SampleWs sample_ws(int64_t batch, int64_t rows, int64_t vocab, bool bf16) {
@@ -29,7 +31,7 @@ SampleWs sample_ws(int64_t batch, int64_t rows, int64_t vocab, bool bf16) {
   const int64_t pieces = vocab / (bf16 ? 8 : 4) + 2;  // a row may begin and end inside one
   w.granules = granules_of(rows, pieces);
   w.chunks = (int)((pieces + w.granules - 1) / w.granules);
-  size_t at = round_up(kMaxRows * sizeof(uint32_t), kAlign);
+  size_t at = 2 * kCounters;
   auto take = [&](size_t bytes) {
     const size_t x = at;
     at += round_up(bytes, kAlign);
@@ -37,6 +39,8 @@ SampleWs sample_ws(int64_t batch, int64_t rows, int64_t vocab, bool bf16) {
   };
   const size_t n = (size_t)rows * w.chunks;
   w.row = take((size_t)rows * sizeof(SampleRow));
+  w.plan = take((size_t)rows * sizeof(SamplePlan));
+  w.list = take((size_t)rows * kSampleList * 2 * sizeof(uint64_t));
   w.c_top = take(n * sizeof(float));
   w.c_best = take(n * sizeof(uint64_t));
   w.c_sum = take(n * sizeof(uint64_t));
@@ -87,6 +91,12 @@ dustin_status place(SampleArgs& a, bool bf16, void* ws, size_t ws_bytes) {
   a.granules = w.granules;
   a.chunks = w.chunks;
   a.arrived = reinterpret_cast<uint32_t*>(base);
+  a.listed = reinterpret_cast<uint32_t*>(base + kCounters);
+  const int64_t rows = (int64_t)a.batch * a.rows_per_seq;
+  a.parts = (int32_t)(rows >= 512 ? 1 : (512 + rows - 1) / rows);
+  if (a.parts > w.chunks) a.parts = w.chunks;
+  a.plan = reinterpret_cast<SamplePlan*>(base + w.plan);
+  a.list = reinterpret_cast<uint64_t*>(base + w.list);
   a.row = reinterpret_cast<SampleRow*>(base + w.row);
   a.c_top = reinterpret_cast<float*>(base + w.c_top);
   a.c_best = reinterpret_cast<uint64_t*>(base + w.c_best);

@@ -5,10 +5,11 @@
 // those the fewest whose weights reach top_p of the sum, of those the ones whose weight is at least min_p of the
 // largest.  It is described by the rank of its last token.  Three kernels:
 //   chunks  every workgroup takes a piece of a row: its largest logit, the sum of its weights against that, and where
-//           a filter needs it a histogram of counts and sums over quarter octaves of the weight
-//   rows    one workgroup a row joins these, finds the quarter octave in which the kept set ends, and reads the row
-//           again for the tokens that it has to rank: where all that may be kept are few, it holds them in LDS, ranks
-//           them and draws; otherwise it ranks those of the last quarter octave by histograms of ever finer ranges
+//           a filter needs it a histogram of counts and sums over eighths of octaves of the weight; the last one of a
+//           row joins these and finds the eighth in which the kept set ends
+//   rows    the tokens that have to be ranked are listed: all that may be kept where those are few (each is then
+//           compared with each), otherwise those of the last eighth (ranked by histograms of ever finer ranges); where
+//           even these are many, one workgroup reads the row as often as it takes
 //   rest    (verification) what is left of the target's distribution after the first rejected draft, and the draw
 // Weights are computed in 64-bit floating point and summed as integers, so results do not depend on the order of
 // work; see sample.hpp.
@@ -18,11 +19,11 @@ namespace dustin {
 
 namespace {
 
-constexpr int kChunkThreads = 256;
+constexpr int kChunkThreads = 512;
+static_assert(kSampleBins <= kChunkThreads, "a thread to a bin");
 constexpr int kRowThreads = 1024;
 constexpr int kRowWaves = kRowThreads / kWave;
-constexpr int kFew = 1024;   // tokens ranked by comparing each with each
-constexpr int kList = 4096;  // tokens of the last quarter octave held in LDS
+constexpr int kFew = kSampleFew, kList = kSampleList;
 
 // 2^d for -46 <= d <= 0, within a few units of 2^-53: 2^d = 2^n 2^f, |f| <= 1/2, and the Taylor series of e^(f ln 2)
 // to the 12th power (the next term is below 2^-52).
@@ -61,7 +62,9 @@ struct Settings {
     const float mm = a.min_p ? a.min_p[b] : a.s_min_p;
     m = mm > 0.f ? (mm < 1.f ? (double)mm : 1.0) : 0.0;
   }
-  __device__ __forceinline__ bool filters() const { return !greedy && (k > 0 || p < 1.0); }
+  __device__ __forceinline__ bool filters() const { return !greedy && (k > 0 || p < 1.0 || m > 0.0); }
+  // all that may be kept is few whatever the weights are: the histogram holds counts alone
+  __device__ __forceinline__ bool counts_do() const { return k > 0 && k <= kFew / 2; }
 };
 
 // Weight of logit x in a row (or chunk) whose largest is top.
@@ -85,8 +88,76 @@ __device__ __forceinline__ float logit_of_key(uint32_t key) {
 }
 __device__ __forceinline__ float logit_of_rank(uint64_t r) { return logit_of_key(~(uint32_t)(r >> kSampleIdxBits)); }
 
-// Quarter octave of a logit (an integer, ascending with it).
-__device__ __forceinline__ double octave(float x, double scale) { return __builtin_floor((double)x * scale * 4.0); }
+// Logits of the ranks from lo to hi lie in [bottom(hi), ceiling(lo)].
+__device__ __forceinline__ float ceiling_of(uint64_t lo) {
+  const uint32_t key = ~(uint32_t)(lo >> kSampleIdxBits);
+  return key >= 0xff800000u ? INFINITY : logit_of_key(key);
+}
+__device__ __forceinline__ float bottom_of(uint64_t hi) {
+  const uint32_t key = ~(uint32_t)(hi >> kSampleIdxBits);
+  return key <= 0x007fffffu ? -INFINITY : logit_of_key(key);
+}
+__device__ __forceinline__ uint64_t whole_key(uint32_t key) {
+  return ((uint64_t)~key << kSampleIdxBits) | (kSampleMaxVocab - 1);
+}
+
+// Eighth of an octave that a logit's weight falls in (an integer, ascending with it).
+__device__ __forceinline__ double octave(float x, double scale) { return __builtin_floor((double)x * scale * 8.0); }
+
+// The least key, of a row whose largest logit is top, whose logit satisfies a condition that holds from some logit on
+// (of top it does), near a guess of it.
+template <class Holds>
+__device__ __forceinline__ uint32_t least_key(float top, double guess, Holds holds) {
+  const uint32_t most = order_key(top);
+  uint32_t key = order_key((float)guess);
+  key = key > most || guess != guess ? most : key < 0x00800000u ? 0x00800000u : key;
+  uint32_t lo = 0x007fffffu, hi = most;  // holds at hi; at lo not (or it is the least there is)
+  // widening steps from the guess, then halving: a few of each
+  for (uint32_t step = 2; lo < key && key < hi; step *= 8) {
+    if (holds(logit_of_key(key))) {
+      hi = key;
+      key = hi - lo > step ? hi - step : lo;
+    } else {
+      lo = key;
+      key = hi - lo > step ? lo + step : hi;
+    }
+    if (hi - lo <= 16) break;
+  }
+  while (hi - lo > 1) {
+    const uint32_t mid = lo + (hi - lo) / 2;
+    if (holds(logit_of_key(mid))) hi = mid;
+    else lo = mid;
+  }
+  return hi;
+}
+// Least key in eighth of an octave j of the row, counted from its top's, or in a better one.
+__device__ __forceinline__ uint32_t bin_key(float top, double scale, int j) {
+  const double oct = octave(top, scale);
+  return least_key(top, (oct - j) / (8.0 * scale), [&](float x) { return x == top || oct - octave(x, scale) <= j; });
+}
+
+// Values that workgroups of one launch hand to each other go past the caches.
+template <class V>
+__device__ __forceinline__ void put(V* p, V x) {
+  __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <class V>
+__device__ __forceinline__ V get(const V* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// Whether this workgroup is the last of n to come here (its writes by put() being complete), for every thread; the
+// counter is back at zero then.
+__device__ __forceinline__ bool arrive_last(uint32_t* counter, uint32_t n, int* sm) {
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): the writes have reached memory
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const uint32_t before = n == 1 ? 0 : __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *sm = before == n - 1;
+    if (before == n - 1 && n > 1) put(counter, 0u);
+  }
+  __syncthreads();
+  return *sm;
+}
 
 // A row in 16-byte pieces: piece g holds tokens first(g) .. first(g) + n - 1.  Logits that are NaN, and tokens outside
 // the row, come as -infinity.
@@ -179,45 +250,64 @@ __device__ __forceinline__ uint64_t block_before(uint64_t x, uint64_t* sm, uint6
   return base + incl - x;
 }
 
-template <bool kBf16>
+// What a chunk's sums of weights are multiplied by to be against the row's largest logit.
+__device__ __forceinline__ double rescaled(float c_top, float top, double scale) {
+  if (c_top == top) return 1.0;
+  const double d = ((double)c_top - (double)top) * scale;
+  return d > -46.0 ? exp2_f64(d) : d > -110.0 ? exp2_f64(d + 64.0) * 0x1p-64 : 0.0;
+}
+__device__ __forceinline__ uint64_t scaled(uint64_t sum, double factor) {
+  return factor == 1.0 ? sum : (uint64_t)((double)sum * factor);
+}
+
+template <bool kBf16, bool kDraw>
 __global__ __launch_bounds__(kChunkThreads) void sample_chunk_kernel(SampleArgs a) {
   constexpr int n = RowReader<kBf16>::n, kMost = kRowThreads / kChunkThreads;  // pieces of a thread, at most
-  __shared__ unsigned long long sm_sum[kChunkThreads / kWave][kSampleBins];
-  __shared__ uint32_t sm_cnt[kChunkThreads / kWave][kSampleBins];
-  __shared__ uint64_t sm_red[kChunkThreads / kWave];
-  const int chunk = blockIdx.x, r = blockIdx.y, wave = threadIdx.x / kWave;
+  constexpr int kWaves = kChunkThreads / kWave;
+  __shared__ unsigned long long sm_sum[kWaves][kSampleBins];
+  __shared__ uint32_t sm_cnt[kWaves][kSampleBins];
+  __shared__ uint64_t sm_red[kWaves];
+  __shared__ double sm_factor[kSampleMaxChunks];
+  __shared__ int sm_off[kSampleMaxChunks];
+  __shared__ int sm_int;
+  const int chunk = blockIdx.x, r = blockIdx.y, tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
   const int b = r / a.rows_per_seq, t = r - b * a.rows_per_seq;
   if (a.n_query && t >= a.n_query[b]) return;
   const RowReader<kBf16> row(a, b, t);
   const Settings s(a, b);
   float x[kMost][n];
-  uint64_t best = ~0ull;
 #pragma unroll
   for (int j = 0; j < kMost; ++j) {
-    const int g = j * kChunkThreads + threadIdx.x;
+    const int g = j * kChunkThreads + tid;
 #pragma unroll
     for (int e = 0; e < n; ++e) x[j][e] = -INFINITY;
     if (g < a.granules) row.read(chunk * a.granules + g, x[j]);
   }
-#pragma unroll
-  for (int j = 0; j < kMost; ++j)
-#pragma unroll
-    for (int e = 0; e < n; ++e) {
-      const int i = row.first(chunk * a.granules + j * kChunkThreads + (int)threadIdx.x) + e;
-      const uint64_t k = rank_of(x[j][e], i & (kSampleMaxVocab - 1));
-      best = x[j][e] != -INFINITY && k < best ? k : best;
-    }
-  const bool filters = s.filters();
+  const bool filters = s.filters(), sums = !s.greedy && !s.counts_do();
   if (filters)
-    for (int i = threadIdx.x & (kWave - 1); i < kSampleBins; i += kWave) {
+    for (int i = lane; i < kSampleBins; i += kWave) {
       sm_sum[wave][i] = 0;
       sm_cnt[wave][i] = 0;
     }
+  // the chunk's best token: its largest logit, then the lowest index that has it
+  float big = -INFINITY;
+#pragma unroll
+  for (int j = 0; j < kMost; ++j)
+#pragma unroll
+    for (int e = 0; e < n; ++e) big = fmaxf(big, x[j][e]);
+  uint64_t best = ~0ull;
+  if (big != -INFINITY) {
+#pragma unroll
+    for (int j = kMost - 1; j >= 0; --j)
+#pragma unroll
+      for (int e = n - 1; e >= 0; --e)
+        if (x[j][e] == big) best = rank_of(big, row.first(chunk * a.granules + j * kChunkThreads + tid) + e);
+  }
   best = wave_min(best);
-  if ((threadIdx.x & (kWave - 1)) == 0) sm_red[wave] = best;
+  if (lane == 0) sm_red[wave] = best;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kChunkThreads / kWave; ++w) best = sm_red[w] < best ? sm_red[w] : best;
+  for (int w = 0; w < kWaves; ++w) best = sm_red[w] < best ? sm_red[w] : best;
   const float top = best == ~0ull ? -INFINITY : logit_of_rank(best);
   uint64_t sum = 0;
   if (!s.greedy && best != ~0ull) {
@@ -226,41 +316,141 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunk_kernel(SampleArgs 
     for (int j = 0; j < kMost; ++j)
 #pragma unroll
       for (int e = 0; e < n; ++e) {
-        const uint64_t w = units(weight(x[j][e], top, s.scale));
-        if (!w) continue;
-        sum += w;
-        if (filters) {
-          const int bin = x[j][e] == top ? 0 : (int)(oct - octave(x[j][e], s.scale));
-          atomicAdd(&sm_sum[wave][bin], (unsigned long long)w);
-          atomicAdd(&sm_cnt[wave][bin], 1u);
+        if (sums) {
+          const uint64_t w = units(weight(x[j][e], top, s.scale));
+          sum += w;
+          if (filters && w) {
+            const int bin = x[j][e] == top ? 0 : (int)(oct - octave(x[j][e], s.scale));
+            atomicAdd(&sm_sum[wave][bin], (unsigned long long)w);
+            atomicAdd(&sm_cnt[wave][bin], 1u);
+          }
+        } else if (x[j][e] != -INFINITY) {
+          const double d = x[j][e] == top ? 0.0 : oct - octave(x[j][e], s.scale);
+          if (d < kSampleBins - 2) atomicAdd(&sm_cnt[wave][(int)d], 1u);
         }
       }
   }
-  sum = block_sum<kChunkThreads / kWave>(sum, sm_red);
-  const int64_t at = (int64_t)r * a.chunks + chunk;
-  if (threadIdx.x == 0) {
-    a.c_top[at] = top;
-    a.c_best[at] = best;
-    a.c_sum[at] = sum;
+  sum = block_sum<kWaves>(sum, sm_red);
+  const int64_t c0 = (int64_t)r * a.chunks, at = c0 + chunk;
+  if (tid == 0) {
+    put(&a.c_top[at], top);
+    put(&a.c_best[at], best);
+    put(&a.c_sum[at], sum);
   }
-  if (filters && threadIdx.x < kSampleBins) {
-    unsigned long long h = 0;
+  if (filters && tid < kSampleBins) {
+    uint64_t h = 0;
     uint32_t c = 0;
 #pragma unroll
-    for (int w = 0; w < kChunkThreads / kWave; ++w) {
-      h += sm_sum[w][threadIdx.x];
-      c += sm_cnt[w][threadIdx.x];
+    for (int w = 0; w < kWaves; ++w) {
+      h += sm_sum[w][tid];
+      c += sm_cnt[w][tid];
     }
-    a.h_sum[at * kSampleBins + threadIdx.x] = h;
-    a.h_cnt[at * kSampleBins + threadIdx.x] = c;
+    if (sums) put(&a.h_sum[at * kSampleBins + tid], h);
+    put(&a.h_cnt[at * kSampleBins + tid], c);
   }
-}
+  if (!arrive_last(&a.arrived[r], a.chunks, &sm_int)) return;
 
-// A chunk's sum of weights, in units of the row's.
-__device__ __forceinline__ uint64_t rescaled(uint64_t sum, float c_top, float top, double scale) {
-  if (c_top == top) return sum;
-  const double d = ((double)c_top - (double)top) * scale;
-  return d > -110.0 ? (uint64_t)((double)sum * (d > -46.0 ? exp2_f64(d) : exp2_f64(d + 64.0) * 0x1p-64)) : 0;
+  // ---- the last workgroup of a row joins the chunks and plans the rest
+  uint64_t row_best = ~0ull;
+  for (int c = tid; c < a.chunks; c += kChunkThreads) {
+    const uint64_t y = get(&a.c_best[c0 + c]);
+    row_best = y < row_best ? y : row_best;
+  }
+  row_best = wave_min(row_best);
+  __syncthreads();
+  if (lane == 0) sm_red[wave] = row_best;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) row_best = sm_red[w] < row_best ? sm_red[w] : row_best;
+  const bool none = row_best == ~0ull;
+  const float row_top = none ? -INFINITY : logit_of_rank(row_best);
+  SamplePlan plan{};
+  if (none || s.greedy) {  // nothing to draw from, or nothing to draw
+    if (tid == 0) {
+      a.plan[r] = plan;
+      a.row[r] = {none ? 0 : row_best, none ? 0 : 1ull << kSampleFrac, row_top};
+      if constexpr (kDraw) a.token[b] = none ? -1 : (int)(row_best & (kSampleMaxVocab - 1));
+    }
+    return;
+  }
+  const double oct = octave(row_top, s.scale);
+  uint64_t all_sum = 0;
+  for (int c = tid; c < a.chunks; c += kChunkThreads) {
+    const float c_top = get(&a.c_top[c0 + c]);
+    const double off = c_top == row_top ? 0.0 : oct - octave(c_top, s.scale);
+    sm_off[c] = off < kSampleBins ? (int)off : kSampleBins;
+    sm_factor[c] = rescaled(c_top, row_top, s.scale);
+    if (sums) all_sum += scaled(get(&a.c_sum[c0 + c]), sm_factor[c]);
+  }
+  if (!filters) {
+    all_sum = block_sum<kWaves>(all_sum, sm_red);
+    plan.mode = kDraw ? kRowWhole : kRowDone;
+    plan.all_sum = all_sum;
+    if (tid == 0) {
+      a.plan[r] = plan;
+      a.row[r] = {~0ull, all_sum, row_top};
+    }
+    return;
+  }
+  __syncthreads();
+  uint64_t my_cnt = 0, my_sum = 0;
+  if (tid < kSampleBins) {
+#pragma unroll 8
+    for (int c = 0; c < a.chunks; ++c) {
+      const int bin = tid - sm_off[c];
+      const int64_t h = (c0 + c) * kSampleBins + (bin < 0 ? 0 : bin);
+      const uint32_t y = get(&a.h_cnt[h]);
+      my_cnt += bin < 0 ? 0 : y;
+      if (sums) {
+        const uint64_t z = get(&a.h_sum[h]);
+        my_sum += bin < 0 ? 0 : scaled(z, sm_factor[c]);
+      }
+    }
+  }
+  uint64_t all_cnt;
+  const uint64_t cnt_before = block_before<kWaves>(my_cnt, sm_red, all_cnt);
+  const uint64_t sum_before = block_before<kWaves>(my_sum, sm_red, all_sum);
+  // the eighth of an octave in which the kept set ends, by count or sum, and by min_p
+  const bool by_count = s.k > 0 && (uint64_t)s.k < all_cnt;
+  double target = by_count ? (double)s.k : s.p * (double)all_sum;
+  if (!by_count && s.counts_do()) target = (double)all_cnt;  // (fewer tokens than top_k: they are few)
+  const bool count_scale = by_count || s.counts_do();
+  __syncthreads();
+  if (tid == 0) sm_int = kSampleBins - 1;
+  __syncthreads();
+  if (tid < kSampleBins && my_cnt &&
+      (count_scale ? (double)(cnt_before + my_cnt) : (double)(sum_before + my_sum)) >= target)
+    atomicMin(&sm_int, tid);
+  __syncthreads();
+  int bin = sm_int;
+  plan.least = ~0ull;
+  if (s.m > 0.0) {
+    const float m = (float)s.m;
+    plan.least = whole_key(least_key(row_top, (double)row_top + (double)__log2f(m) / s.scale,
+                                     [&](float x) { return weight(x, row_top, s.scale) >= s.m; }));
+    const float x = logit_of_rank(plan.least);
+    const int bin_m = x == row_top ? 0 : (int)(oct - octave(x, s.scale));
+    if (bin_m < bin) {
+      bin = bin_m;
+      target = -1.0;
+    }
+  }
+  if (tid == bin) {  // (a eighth of an octave that only min_p names may hold no token)
+    const uint64_t upto = cnt_before + my_cnt;
+    const bool p_of_k = by_count && s.p < 1.0;  // top_p of a sum that the top_k leave
+    plan.mode = upto <= kFew || s.counts_do() ? kRowFew : my_cnt <= kList && !p_of_k ? kRowList : kRowRead;
+    plan.bin = bin;
+    plan.hi = whole_key(bin_key(row_top, s.scale, bin));
+    plan.lo = plan.mode == kRowList && bin > 0 ? whole_key(bin_key(row_top, s.scale, bin - 1)) + 1 : 0;
+    plan.before_cnt = cnt_before;
+    plan.before_sum = sum_before;
+    plan.all_sum = all_sum;
+    plan.target = target;
+    plan.by_count = by_count;
+    if (plan.mode == kRowFew && upto > kFew) plan.mode = kRowRead;
+    a.plan[r] = plan;
+    a.row[r] = {0, 0, row_top};
+  }
 }
 
 // Of the tokens of a chunk (one piece to a thread) with rank at most `last`, the one at which the running sum of
@@ -315,314 +505,211 @@ __device__ int draw_chunk(const SampleArgs& a, float u, Value value, uint64_t* s
   return *sm_chunk;
 }
 
+// What the plan of a row leaves: up to `parts` workgroups list the tokens to be ranked, the last of them ranks them and
+// draws.
 template <bool kBf16, bool kDraw>
 __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
   constexpr int n = RowReader<kBf16>::n;
   __shared__ uint64_t sm_rank[kList];
   __shared__ uint64_t sm_w[kList];
-  __shared__ unsigned long long sm_sum[1024];  // histogram: of quarter octaves, then of ranges of ranks
+  __shared__ unsigned long long sm_sum[1024];  // a histogram of ranges of ranks
   __shared__ uint32_t sm_cnt[1024];
   __shared__ unsigned long long sm_chunk_sum[kSampleMaxChunks];
+  __shared__ double sm_factor[kSampleMaxChunks];
+  __shared__ int sm_off[kSampleMaxChunks];
   __shared__ uint64_t sm_red[kRowWaves], sm_u64[4];
   __shared__ int sm_int[2];
-  __shared__ uint32_t sm_n;
-  const int r = blockIdx.x, tid = threadIdx.x;
+  const int r = blockIdx.y, tid = threadIdx.x;
   const int b = r / a.rows_per_seq, t = r - b * a.rows_per_seq;
   if (a.n_query && t >= a.n_query[b]) return;
+  const SamplePlan plan = a.plan[r];
+  const bool lists = plan.mode == kRowFew || plan.mode == kRowList;
+  if (plan.mode == kRowDone || (!lists && blockIdx.x > 0)) return;
+  const float top = a.row[r].top;
   const RowReader<kBf16> row(a, b, t);
   const Settings s(a, b);
   const int64_t c0 = (int64_t)r * a.chunks;
   const int pieces = a.granules * a.chunks;
-
-  // ---- the row's best token
-  uint64_t best = tid < a.chunks ? a.c_best[c0 + tid] : ~0ull;
-  best = wave_min(best);
-  if ((tid & (kWave - 1)) == 0) sm_red[tid / kWave] = best;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kRowWaves; ++w) best = sm_red[w] < best ? sm_red[w] : best;
-  if (best == ~0ull || s.greedy) {  // nothing to draw from, or nothing to draw
-    if (tid == 0) {
-      const bool none = best == ~0ull;
-      a.row[r] = {none ? 0 : best, none ? 0 : 1ull << kSampleFrac, none ? -INFINITY : logit_of_rank(best)};
-      if constexpr (kDraw) a.token[b] = none ? -1 : (int)(best & (kSampleMaxVocab - 1));
-    }
-    return;
-  }
-  const float top = logit_of_rank(best);
   auto units_of = [&](float x) { return units(weight(x, top, s.scale)); };
-  // calls f(x, i) for every token of the row whose rank lies in [lo, hi]
-  auto each = [&](uint64_t lo, uint64_t hi, auto f) {
-    const uint32_t key_hi = ~(uint32_t)(lo >> kSampleIdxBits), key_lo = ~(uint32_t)(hi >> kSampleIdxBits);
-    for (int g = tid; g < pieces; g += kRowThreads) {
+  // calls f(rank, units) for every token of pieces [g0, g1) that has any and whose rank lies in [lo, hi]
+  auto each = [&](int g0, int g1, uint64_t lo, uint64_t hi, auto f) {
+    const float x_hi = ceiling_of(lo), x_lo = bottom_of(hi);
+    for (int g = g0 + tid; g < g1; g += kRowThreads) {
       float x[n];
       row.read(g, x);
+      bool any = false;
 #pragma unroll
-      for (int e = 0; e < n; ++e) {
-        const uint32_t k = order_key(x[e]);
-        if (x[e] != -INFINITY && k >= key_lo && k <= key_hi) {
+      for (int e = 0; e < n; ++e) any |= x[e] >= x_lo && x[e] <= x_hi;
+      if (!any) continue;
+#pragma unroll
+      for (int e = 0; e < n; ++e)
+        if (x[e] >= x_lo && x[e] <= x_hi && x[e] != -INFINITY) {
           const uint64_t c = rank_of(x[e], row.first(g) + e);
-          if (c >= lo && c <= hi) f(x[e], c);
+          const uint64_t w = c >= lo && c <= hi ? units_of(x[e]) : 0;
+          if (w) f(c, w);
         }
+    }
+  };
+  int m = 0;  // tokens in the list
+  if (lists) {
+    const int share = (pieces + a.parts - 1) / a.parts;
+    uint64_t* list = a.list + (int64_t)r * kList * 2;
+    each(blockIdx.x * share, min(pieces, (int)(blockIdx.x + 1) * share), plan.lo, plan.hi, [&](uint64_t c, uint64_t w) {
+      const uint32_t at = __hip_atomic_fetch_add(&a.listed[r], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (at < kList) {
+        put(list + 2 * at, c);
+        put(list + 2 * at + 1, w);
       }
+    });
+    if (!arrive_last(&a.arrived[r], a.parts, &sm_int[0])) return;
+    m = min((int)get(&a.listed[r]), kList);
+    for (int j = tid; j < m; j += kRowThreads) {
+      sm_rank[j] = get(list + 2 * j);
+      sm_w[j] = get(list + 2 * j + 1);
     }
-  };
-  // least key whose logit satisfies a condition that holds from some logit on
-  auto least_key = [&](auto holds) {
-    uint32_t lo = 0, hi = order_key(top);  // holds(hi)
-    while (lo < hi) {
-      const uint32_t mid = lo + (hi - lo) / 2;
-      if (holds(logit_of_key(mid))) hi = mid;
-      else lo = mid + 1;
+    __syncthreads();
+    if (tid == 0) put(&a.listed[r], 0u);
+  }
+  if (plan.mode == kRowFew) {
+    // ---- few: each compared with each
+    m = min(m, kFew);
+    int share = 64;  // threads to a token
+    while (share * m > kRowThreads) share >>= 1;
+    const int e = tid / share, part = tid % share;
+    const bool mine = e < m;
+    const uint64_t c = mine ? sm_rank[e] : 0, w = mine ? sm_w[e] : 0;
+    uint64_t place = 0, before = 0;
+    if (mine)
+      for (int j = part; j < m; j += share)
+        if (sm_rank[j] < c) {
+          ++place;
+          before += sm_w[j];
+        }
+    for (int d = 1; d < share; d *= 2) {
+      place += shfl_xor_u64(place, d);
+      before += shfl_xor_u64(before, d);
     }
-    return lo;
-  };
-  auto whole_key = [](uint32_t key) { return ((uint64_t)~key << kSampleIdxBits) | (kSampleMaxVocab - 1); };
+    bool kept = mine && (s.k == 0 || place < (uint64_t)s.k);
+    // (without a top_k the list need not hold all that the sum is over)
+    const uint64_t z_k = s.counts_do() || plan.by_count ? block_sum<kRowWaves>(kept && part == 0 ? w : 0, sm_red) : plan.all_sum;
+    if (s.p < 1.0) kept &= place == 0 || (double)before < s.p * (double)z_k;
+    kept &= place == 0 || weight(logit_of_rank(c), top, s.scale) >= s.m;
+    const uint64_t z = block_sum<kRowWaves>(kept && part == 0 ? w : 0, sm_red);
+    if (tid == 0) sm_u64[3] = 0;
+    __syncthreads();
+    if (kept && part == 0) atomicMax(reinterpret_cast<unsigned long long*>(&sm_u64[3]), (unsigned long long)c);
+    if (mine && part == 0) sm_w[e] = kept ? w : 0;
+    __syncthreads();
+    if constexpr (kDraw) {
+      float u = a.u[b];
+      u = u > 0.f ? u : 0.f;
+      uint64_t target = (uint64_t)((double)u * (double)z);
+      if (target >= z) target = z - 1;
+      const uint32_t i = (uint32_t)c & (kSampleMaxVocab - 1);
+      uint64_t run = 0;
+      if (kept)
+        for (int j = part; j < m; j += share)
+          if (((uint32_t)sm_rank[j] & (kSampleMaxVocab - 1)) < i) run += sm_w[j];
+      for (int d = 1; d < share; d *= 2) run += shfl_xor_u64(run, d);
+      if (kept && part == 0 && run <= target && target < run + w) a.token[b] = (int)i;
+    }
+    if (tid == 0) a.row[r] = {sm_u64[3], z, top};
+    return;
+  }
 
-  uint64_t last = ~0ull;  // rank of the last kept token
-  int last_bin = -1;      // its quarter octave, with a histogram
-  if (s.filters()) {
-    // ---- histogram of the row
-    const double oct = octave(top, s.scale);
-    for (int i = tid; i < 1024; i += kRowThreads) {
-      sm_sum[i] = 0;
-      sm_cnt[i] = 0;
+  // ---- many: the last token by ever finer ranges of ranks
+  uint64_t last = ~0ull;  // its rank
+  auto each_token = [&](uint64_t lo, uint64_t hi, auto f) {
+    if (plan.mode == kRowList) {
+      for (int j = tid; j < m; j += kRowThreads)
+        if (sm_rank[j] >= lo && sm_rank[j] <= hi) f(sm_rank[j], sm_w[j]);
+    } else {
+      each(0, pieces, lo, hi, f);
     }
-    if (tid == 0) sm_n = 0;
-    __syncthreads();
-    for (int e = tid; e < a.chunks * kSampleBins; e += kRowThreads) {
-      const int c = e / kSampleBins, bin = e - c * kSampleBins;
-      const uint32_t cnt = a.h_cnt[c0 * kSampleBins + e];
-      const float c_top = a.c_top[c0 + c];
-      const double off = c_top == top ? 0.0 : oct - octave(c_top, s.scale);
-      if (cnt && off + bin < kSampleBins) {
-        atomicAdd(&sm_cnt[(int)off + bin], cnt);
-        atomicAdd(&sm_sum[(int)off + bin], (unsigned long long)rescaled(a.h_sum[c0 * kSampleBins + e], c_top, top, s.scale));
-      }
-    }
-    __syncthreads();
-    uint64_t all_cnt, all_sum;
-    const uint64_t my_cnt = tid < kSampleBins ? sm_cnt[tid] : 0, my_sum = tid < kSampleBins ? sm_sum[tid] : 0;
-    const uint64_t cnt_before = block_before<kRowWaves>(my_cnt, sm_red, all_cnt);
-    const uint64_t sum_before = block_before<kRowWaves>(my_sum, sm_red, all_sum);
-    // ends of quarter octaves: a token lies in bin j or a better one iff its key is at least bin_key(j)
-    auto bin_key = [&](int j) { return least_key([&](float x) { return oct - octave(x, s.scale) <= j; }); };
-    // the first bin whose running count (or sum) reaches a target; the counts and sums before it and in it
-    struct Bin {
-      int j;
-      uint64_t cnt, sum, in;
-    };
-    auto find_bin = [&](bool by_sum, double target) {
+  };
+  // the first token of ranks lo .. hi at which the running count (or sum), from what is before them, reaches the
+  // target, else the last there is; the sum up to it
+  auto find_token = [&](uint64_t lo, uint64_t hi, uint64_t cnt_b, uint64_t sum_b, bool by_sum, double target,
+                        uint64_t& sum) {
+    for (;;) {
+      const int bits = hi == lo ? 0 : 64 - __clzll((long long)(hi - lo));
+      const int shift = bits > 10 ? bits - 10 : 0;
       __syncthreads();
-      if (tid == 0) sm_int[0] = kSampleBins - 1;
-      __syncthreads();
-      const double reach = by_sum ? (double)(sum_before + my_sum) : (double)(cnt_before + my_cnt);
-      if (tid < kSampleBins && my_cnt && reach >= target) atomicMin(&sm_int[0], tid);
-      __syncthreads();
-      const int j = sm_int[0];
-      if (tid == j) {
-        sm_u64[0] = cnt_before;
-        sm_u64[1] = sum_before;
-        sm_u64[2] = my_cnt;
+      sm_sum[tid] = 0;
+      sm_cnt[tid] = 0;
+      if (tid == 0) {
+        sm_int[0] = 1 << 20;
+        sm_int[1] = 0;
       }
       __syncthreads();
-      return Bin{j, sm_u64[0], sm_u64[1], sm_u64[2]};
-    };
-    const bool by_count = s.k > 0 && (uint64_t)s.k < all_cnt;
-    Bin bin = by_count ? find_bin(false, s.k) : find_bin(true, s.p * (double)all_sum);
-    if (bin.cnt + bin.in <= kFew) {
-      // ---- few: all that may be kept, in LDS, each compared with each
-      each(0, whole_key(bin_key(bin.j)), [&](float x, uint64_t c) {
-        const uint64_t w = units_of(x);
-        if (!w) return;
-        const uint32_t at = atomicAdd(&sm_n, 1u);
-        if (at < kFew) {
-          sm_rank[at] = c;
-          sm_w[at] = w;
-        }
+      each_token(lo, hi, [&](uint64_t c, uint64_t w) {
+        const int j = (int)((c - lo) >> shift);
+        atomicAdd(&sm_cnt[j], 1u);
+        atomicAdd(&sm_sum[j], (unsigned long long)w);
       });
       __syncthreads();
-      const int m = min((int)sm_n, kFew);
-      int share = 64;  // threads to a token
-      while (share * m > kRowThreads) share >>= 1;
-      const int e = tid / share, part = tid % share;
-      const bool mine = e < m;
-      const uint64_t c = mine ? sm_rank[e] : 0, w = mine ? sm_w[e] : 0;
-      uint64_t place = 0, before = 0;
-      if (mine)
-        for (int j = part; j < m; j += share)
-          if (sm_rank[j] < c) {
-            ++place;
-            before += sm_w[j];
-          }
-      for (int d = 1; d < share; d *= 2) {
-        place += shfl_xor_u64(place, d);
-        before += shfl_xor_u64(before, d);
-      }
-      bool kept = mine && (s.k == 0 || place < (uint64_t)s.k);
-      const uint64_t z_k = by_count ? block_sum<kRowWaves>(kept && part == 0 ? w : 0, sm_red) : all_sum;
-      if (s.p < 1.0) kept &= place == 0 || (double)before < s.p * (double)z_k;
-      kept &= place == 0 || weight(logit_of_rank(c), top, s.scale) >= s.m;
-      const uint64_t z = block_sum<kRowWaves>(kept && part == 0 ? w : 0, sm_red);
-      if (tid == 0) {
-        sm_u64[3] = 0;
-        sm_int[1] = -1;
-      }
-      __syncthreads();
-      if (kept && part == 0) atomicMax(reinterpret_cast<unsigned long long*>(&sm_u64[3]), (unsigned long long)c);
-      if (mine && part == 0) sm_w[e] = kept ? w : 0;
-      __syncthreads();
-      if constexpr (kDraw) {
-        float u = a.u[b];
-        u = u > 0.f ? u : 0.f;
-        uint64_t target = (uint64_t)((double)u * (double)z);
-        if (target >= z) target = z - 1;
-        const uint32_t i = (uint32_t)c & (kSampleMaxVocab - 1);
-        uint64_t run = 0;
-        if (kept)
-          for (int j = part; j < m; j += share)
-            if (((uint32_t)sm_rank[j] & (kSampleMaxVocab - 1)) < i) run += sm_w[j];
-        for (int d = 1; d < share; d *= 2) run += shfl_xor_u64(run, d);
-        if (kept && part == 0 && run <= target && target < run + w) a.token[b] = (int)i;
-      }
-      if (tid == 0) a.row[r] = {sm_u64[3], z, top};
-      return;
-    }
-    // ---- many: the last token by ever finer ranges of ranks
-    uint64_t list_lo = 1, list_hi = 0;  // ranks whose tokens are in the list
-    int list_n = 0;
-    auto each_of = [&](uint64_t lo, uint64_t hi, auto f) {  // f(rank, units)
-      if (list_lo <= lo && hi <= list_hi) {
-        for (int j = tid; j < list_n; j += kRowThreads)
-          if (sm_rank[j] >= lo && sm_rank[j] <= hi) f(sm_rank[j], sm_w[j]);
-      } else {
-        each(lo, hi, [&](float x, uint64_t c) {
-          const uint64_t w = units_of(x);
-          if (w) f(c, w);
-        });
-      }
-    };
-    // the first token, from bin `at` on, at which the running count (sum) reaches the target; sum up to it
-    auto find_token = [&](const Bin& at, bool by_sum, double target, uint64_t& sum) {
-      uint64_t lo = at.j == 0 ? 0 : whole_key(bin_key(at.j - 1)) + 1, hi = whole_key(bin_key(at.j));
-      uint64_t cnt_b = at.cnt, sum_b = at.sum;
-      if (!(list_lo <= lo && hi <= list_hi) && at.in <= kList) {
-        __syncthreads();
-        if (tid == 0) sm_n = 0;
-        __syncthreads();
-        each(lo, hi, [&](float x, uint64_t c) {
-          const uint64_t w = units_of(x);
-          if (!w) return;
-          const uint32_t j = atomicAdd(&sm_n, 1u);
-          if (j < kList) {
-            sm_rank[j] = c;
-            sm_w[j] = w;
-          }
-        });
-        __syncthreads();
-        list_n = min((int)sm_n, kList);
-        list_lo = lo;
-        list_hi = hi;
-      }
-      for (;;) {
-        const int bits = 64 - __clzll((long long)(hi - lo));  // hi > lo, or 0
-        const int shift = hi == lo ? 0 : bits > 10 ? bits - 10 : 0;
-        __syncthreads();
-        sm_sum[tid] = 0;
-        sm_cnt[tid] = 0;
-        if (tid == 0) sm_int[0] = 1 << 20;
-        __syncthreads();
-        each_of(lo, hi, [&](uint64_t c, uint64_t w) {
-          const int j = (int)((c - lo) >> shift);
-          atomicAdd(&sm_cnt[j], 1u);
-          atomicAdd(&sm_sum[j], (unsigned long long)w);
-        });
-        __syncthreads();
-        const uint64_t oc = sm_cnt[tid], os = sm_sum[tid];
-        uint64_t x;
-        const uint64_t cb = cnt_b + block_before<kRowWaves>(oc, sm_red, x);
-        const uint64_t sb = sum_b + block_before<kRowWaves>(os, sm_red, x);
-        if (oc && (by_sum ? (double)(sb + os) : (double)(cb + oc)) >= target) atomicMin(&sm_int[0], tid);
-        __syncthreads();
-        if (sm_int[0] == 1 << 20) {  // (sums of the histogram and of the tokens differ in the last place)
-          __syncthreads();
-          if (tid == 0) sm_int[0] = -1;
-          __syncthreads();
-          if (oc) atomicMax(&sm_int[0], tid);
-          __syncthreads();
-        }
-        const int j = max(sm_int[0], 0);
-        if (tid == j) {
-          sm_u64[0] = cb;
-          sm_u64[1] = sb;
-          sm_u64[2] = sb + os;
-        }
-        __syncthreads();
-        cnt_b = sm_u64[0];
-        sum_b = sm_u64[1];
-        sum = sm_u64[2];
-        lo += (uint64_t)j << shift;
-        if (shift == 0) return lo;
-        const uint64_t end = lo + ((1ull << shift) - 1);
-        hi = end < hi ? end : hi;
-      }
-    };
-    uint64_t z_k = all_sum;
-    last_bin = kSampleBins - 1;
-    if (by_count) {
-      last = find_token(bin, false, s.k, z_k);
-      last_bin = bin.j;
-    }
-    if (s.p < 1.0) {
-      if (by_count) {  // the histogram of ranges has taken the place of that of quarter octaves: both are in registers
-        bin = find_bin(true, s.p * (double)z_k);
-      }
+      const uint64_t oc = sm_cnt[tid], os = sm_sum[tid];
       uint64_t x;
-      const uint64_t at = find_token(bin, true, s.p * (double)z_k, x);
-      if (at < last) {
-        last = at;
-        last_bin = bin.j;
+      const uint64_t cb = cnt_b + block_before<kRowWaves>(oc, sm_red, x);
+      const uint64_t sb = sum_b + block_before<kRowWaves>(os, sm_red, x);
+      if (oc && (by_sum ? (double)(sb + os) : (double)(cb + oc)) >= target) atomicMin(&sm_int[0], tid);
+      if (oc) atomicMax(&sm_int[1], tid);
+      __syncthreads();
+      const int j = min(sm_int[0], sm_int[1]);
+      if (tid == j) {
+        sm_u64[0] = cb;
+        sm_u64[1] = sb;
+        sm_u64[2] = sb + os;
       }
+      __syncthreads();
+      cnt_b = sm_u64[0];
+      sum_b = sm_u64[1];
+      sum = sm_u64[2];
+      lo += (uint64_t)j << shift;
+      if (shift == 0) return lo;
+      const uint64_t end = lo + ((1ull << shift) - 1);
+      hi = end < hi ? end : hi;
+    }
+  };
+  uint64_t sum;
+  if (plan.mode == kRowList) {
+    last = plan.target < 0.0 ? plan.least
+                             : find_token(plan.lo, plan.hi, plan.before_cnt, plan.before_sum, !plan.by_count, plan.target, sum);
+  } else if (plan.mode == kRowRead) {
+    // no more than 2^-45.5 of the largest weight: every token that has any
+    const uint64_t end = whole_key(bin_key(top, s.scale, kSampleBins - 1));
+    uint64_t z = s.counts_do() ? 0 : plan.all_sum;
+    if (s.k > 0) last = find_token(0, end, 0, 0, false, (double)s.k, z);
+    if (s.p < 1.0) {
+      const uint64_t at = find_token(0, end, 0, 0, true, s.p * (double)z, sum);
+      last = at < last ? at : last;
     }
   }
-  if (s.m > 0.0) {
-    const uint64_t at = whole_key(least_key([&](float x) { return weight(x, top, s.scale) >= s.m; }));
-    if (at < last) {
-      last = at;
-      last_bin = s.filters() ? (int)(octave(top, s.scale) - octave(logit_of_rank(at), s.scale)) : -1;
-    }
-  }
+  if (plan.mode != kRowWhole && plan.least < last) last = plan.least;
 
   // ---- sums of the kept weights by chunks
   __syncthreads();
-  if (tid < a.chunks) sm_chunk_sum[tid] = 0;
-  __syncthreads();
-  if (last == ~0ull) {
-    if (tid < a.chunks) sm_chunk_sum[tid] = rescaled(a.c_sum[c0 + tid], a.c_top[c0 + tid], top, s.scale);
-  } else {
-    uint64_t from = 0;  // ranks that the histograms do not give
-    if (last_bin >= 0) {
-      const double oct = octave(top, s.scale);
-      for (int e = tid; e < a.chunks * kSampleBins; e += kRowThreads) {
-        const int c = e / kSampleBins, bin = e - c * kSampleBins;
-        const uint64_t sum = a.h_sum[c0 * kSampleBins + e];
-        const float c_top = a.c_top[c0 + c];
-        const double off = c_top == top ? 0.0 : oct - octave(c_top, s.scale);
-        if (sum && off + bin < last_bin)
-          atomicAdd(&sm_chunk_sum[c], (unsigned long long)rescaled(sum, c_top, top, s.scale));
-      }
-      if (last_bin > 0) {
-        const int j = last_bin - 1;
-        from = whole_key(least_key([&](float x) { return oct - octave(x, s.scale) <= j; })) + 1;
-      }
-    }
-    const uint32_t inv = a.granules * n;
-    each(from, last, [&](float x, uint64_t c) {
-      const uint64_t w = units_of(x);
-      const uint32_t i = (uint32_t)c & (kSampleMaxVocab - 1);
-      if (w) atomicAdd(&sm_chunk_sum[(i + row.skew) / inv], (unsigned long long)w);
-    });
+  for (int c = tid; c < a.chunks; c += kRowThreads) {
+    const float c_top = a.c_top[c0 + c];
+    const double off = c_top == top ? 0.0 : octave(top, s.scale) - octave(c_top, s.scale);
+    sm_off[c] = off < kSampleBins ? (int)off : kSampleBins;
+    sm_factor[c] = rescaled(c_top, top, s.scale);
+    sm_chunk_sum[c] = plan.mode == kRowWhole ? scaled(a.c_sum[c0 + c], sm_factor[c]) : 0;
   }
+  __syncthreads();
+  const int chunk_bits = 31 - __clz(a.granules * n);
+  if (plan.mode == kRowList)
+    for (int e = tid; e < a.chunks * kSampleBins; e += kRowThreads) {
+      const int c = e / kSampleBins, bin = e - c * kSampleBins;
+      if (sm_off[c] + bin >= plan.bin) continue;
+      const uint64_t x = a.h_sum[c0 * kSampleBins + e];
+      if (x) atomicAdd(&sm_chunk_sum[c], (unsigned long long)scaled(x, sm_factor[c]));
+    }
+  if (plan.mode != kRowWhole)
+    each_token(0, last, [&](uint64_t c, uint64_t w) {
+      const uint32_t i = (uint32_t)c & (kSampleMaxVocab - 1);
+      atomicAdd(&sm_chunk_sum[(i + row.skew) >> chunk_bits], (unsigned long long)w);
+    });
   __syncthreads();
   uint64_t z;
   const int chunk = draw_chunk(a, kDraw ? a.u[b] : 0.f, [&](int c) { return (uint64_t)sm_chunk_sum[c]; }, sm_red,
@@ -723,20 +810,12 @@ __global__ __launch_bounds__(kRowThreads) void verify_rest_kernel(SampleArgs a) 
   p_sum = block_sum<kRowWaves>(p_sum, sm_red);
   if (tid == 0) {
     uint64_t* at = a.r_sum + ((int64_t)b * a.chunks + chunk) * 2;
-    __hip_atomic_store(at, r_sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __hip_atomic_store(at + 1, p_sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const uint32_t before = __hip_atomic_fetch_add(a.arrived + b, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
-    sm_int[1] = before == (uint32_t)a.chunks - 1;
+    put(at, r_sum);
+    put(at + 1, p_sum);
   }
-  __syncthreads();
-  if (!sm_int[1]) return;
-  if (tid == 0) {
-    __hip_atomic_store(a.arrived + b, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    a.accepted[b] = kept + 1;
-  }
-  auto stored = [&](int c, int which) {
-    return __hip_atomic_load(a.r_sum + ((int64_t)b * a.chunks + c) * 2 + which, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  };
+  if (!arrive_last(&a.arrived[b], a.chunks, &sm_int[1])) return;
+  if (tid == 0) a.accepted[b] = kept + 1;
+  auto stored = [&](int c, int which) { return get(a.r_sum + ((int64_t)b * a.chunks + c) * 2 + which); };
   const float u = a.u[b];
   uint64_t all;
   int at = draw_chunk(a, u, [&](int c) { return stored(c, 0); }, sm_red, &sm_int[1], &sm_u64[0], all);
@@ -757,8 +836,8 @@ __global__ __launch_bounds__(kRowThreads) void verify_rest_kernel(SampleArgs a) 
 
 template <bool kBf16>
 hipError_t launch_sample_of(const SampleArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL((sample_chunk_kernel<kBf16>), dim3(a.chunks, a.batch), dim3(kChunkThreads), 0, stream, a);
-  hipLaunchKernelGGL((sample_row_kernel<kBf16, true>), dim3(a.batch), dim3(kRowThreads), 0, stream, a);
+  hipLaunchKernelGGL((sample_chunk_kernel<kBf16, true>), dim3(a.chunks, a.batch), dim3(kChunkThreads), 0, stream, a);
+  hipLaunchKernelGGL((sample_row_kernel<kBf16, true>), dim3(a.parts, a.batch), dim3(kRowThreads), 0, stream, a);
   if (a.probs)
     hipLaunchKernelGGL((sample_probs_kernel<kBf16>), dim3((a.vocab + kChunkThreads - 1) / kChunkThreads, a.batch),
                        dim3(kChunkThreads), 0, stream, a);
@@ -768,8 +847,8 @@ hipError_t launch_sample_of(const SampleArgs& a, hipStream_t stream) {
 template <bool kBf16>
 hipError_t launch_verify_of(const SampleArgs& a, hipStream_t stream) {
   const int rows = a.batch * a.rows_per_seq;
-  hipLaunchKernelGGL((sample_chunk_kernel<kBf16>), dim3(a.chunks, rows), dim3(kChunkThreads), 0, stream, a);
-  hipLaunchKernelGGL((sample_row_kernel<kBf16, false>), dim3(rows), dim3(kRowThreads), 0, stream, a);
+  hipLaunchKernelGGL((sample_chunk_kernel<kBf16, false>), dim3(a.chunks, rows), dim3(kChunkThreads), 0, stream, a);
+  hipLaunchKernelGGL((sample_row_kernel<kBf16, false>), dim3(a.parts, rows), dim3(kRowThreads), 0, stream, a);
   hipLaunchKernelGGL((verify_rest_kernel<kBf16>), dim3(a.chunks, a.batch), dim3(kRowThreads), 0, stream, a);
   return hipGetLastError();
 }

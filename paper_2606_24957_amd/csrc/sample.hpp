@@ -14,7 +14,9 @@ constexpr int kSampleMaxVocab = 1 << kSampleIdxBits;
 // integers do not depend on their order, 2^18 tokens stay below 2^62, and a weight is off by at most 2^-45.  Weights
 // below 2^-45 count as zero.
 constexpr int kSampleFrac = 44;
-constexpr int kSampleBins = 184;     // quarter octaves from the largest weight down to 2^-45.5, and one
+constexpr int kSampleBins = 368;     // eighths of octaves from the largest weight down to 2^-45.5, and a few
+constexpr int kSampleFew = 1024;     // tokens ranked by comparing each with each
+constexpr int kSampleList = 4096;    // tokens of a list
 constexpr int kSampleMaxWindow = 64; // tokens of a verification window
 constexpr int kSampleMaxChunks = 264;  // 2^18 fp32 logits in chunks of 256 pieces, wherever the row begins
 
@@ -22,6 +24,24 @@ struct SampleRow {  // what is known of a row once its filters are resolved
   uint64_t last;    // rank of the last kept token (0: none is)
   uint64_t sum;     // of the kept weights
   float top;        // largest logit
+};
+
+// How the rest of a row is done, from its histogram.
+enum SampleMode : int32_t {
+  kRowDone = 0,   // nothing is left to do
+  kRowWhole = 1,  // every token is kept
+  kRowFew = 2,    // all that may be kept are few: ranks lo .. hi
+  kRowList = 3,   // the last kept token's eighth of an octave is ranks lo .. hi
+  kRowRead = 4,   // read the row as often as it takes
+};
+struct SamplePlan {
+  int32_t mode, bin;
+  uint64_t lo, hi;          // ranks of the tokens to list
+  uint64_t before_cnt, before_sum;  // kRowList: tokens of better eighth of an octaves
+  uint64_t all_sum;
+  uint64_t least;           // rank of the last token that min_p keeps (~0: of any)
+  double target;            // kRowList: running count or sum at which the last token is reached (negative: at `least`)
+  int32_t by_count;
 };
 
 struct SampleArgs {
@@ -55,8 +75,12 @@ struct SampleArgs {
   uint64_t* h_sum;    // [rows][chunks][kSampleBins]
   uint32_t* h_cnt;
   SampleRow* row;     // [rows]
+  SamplePlan* plan;   // [rows]
+  uint64_t* list;     // [rows][kSampleList][2] ranks and weights
+  int32_t parts;      // workgroups that list a row's tokens
   uint64_t* r_sum;    // [batch][chunks][2]: sums of what is left of the distribution, and of it whole
-  uint32_t* arrived;  // [batch], zero between calls
+  uint32_t* arrived;  // [rows], zero between calls
+  uint32_t* listed;   // [rows], zero between calls
 };
 
 hipError_t launch_sample(const SampleArgs& a, bool bf16, hipStream_t stream);

@@ -11,19 +11,15 @@ namespace {
 
 constexpr int kMaxRows = 65535;  // rows of logits of a call: a dimension of the launch
 
-// Pieces of 16 bytes to a chunk: as many workgroups as fill the chip, in chunks of no more than 1024.
-int granules_of(int64_t rows, int64_t pieces) {
-  for (int g = 1024; g > 256; g /= 2)
-    if (rows * ((pieces + g - 1) / g) >= 512) return g;
-  return 256;
-}
+// Pieces of 16 bytes to a chunk, a power of two: 512, one to a thread, or 1024 where these fill the chip.
+int granules_of(int64_t rows, int64_t pieces) { return rows * ((pieces + 1023) / 1024) >= 512 ? 1024 : 512; }
 
 constexpr size_t kCounters = (kMaxRows + 1) * sizeof(uint32_t);  // of each kind
 
 // The workspace begins with the arrival and list counters, whatever a call's sizes are.
 struct SampleWs {
   int granules, chunks;
-  size_t row, plan, list, c_top, c_best, c_sum, r_sum, h_cnt, h_sum, total;
+  size_t row, list, c_top, c_best, c_sum, r_sum, h_cnt, h_sum, total;
 };
 
 SampleWs sample_ws(int64_t batch, int64_t rows, int64_t vocab, bool bf16) {
@@ -39,7 +35,6 @@ SampleWs sample_ws(int64_t batch, int64_t rows, int64_t vocab, bool bf16) {
   };
   const size_t n = (size_t)rows * w.chunks;
   w.row = take((size_t)rows * sizeof(SampleRow));
-  w.plan = take((size_t)rows * sizeof(SamplePlan));
   w.list = take((size_t)rows * kSampleList * 2 * sizeof(uint64_t));
   w.c_top = take(n * sizeof(float));
   w.c_best = take(n * sizeof(uint64_t));
@@ -93,9 +88,8 @@ dustin_status place(SampleArgs& a, bool bf16, void* ws, size_t ws_bytes) {
   a.arrived = reinterpret_cast<uint32_t*>(base);
   a.listed = reinterpret_cast<uint32_t*>(base + kCounters);
   const int64_t rows = (int64_t)a.batch * a.rows_per_seq;
-  a.parts = (int32_t)(rows >= 512 ? 1 : (512 + rows - 1) / rows);
+  a.parts = (int32_t)(rows >= 256 ? 1 : 256 / rows);  // (one workgroup to a CU)
   if (a.parts > w.chunks) a.parts = w.chunks;
-  a.plan = reinterpret_cast<SamplePlan*>(base + w.plan);
   a.list = reinterpret_cast<uint64_t*>(base + w.list);
   a.row = reinterpret_cast<SampleRow*>(base + w.row);
   a.c_top = reinterpret_cast<float*>(base + w.c_top);

@@ -19,31 +19,37 @@ namespace dustin {
 
 namespace {
 
-constexpr int kChunkThreads = 512;
-static_assert(kSampleBins <= kChunkThreads, "a thread to a bin");
+constexpr int kChunkThreads = 256;
 constexpr int kRowThreads = 1024;
 constexpr int kRowWaves = kRowThreads / kWave;
 constexpr int kFew = kSampleFew, kList = kSampleList;
+constexpr int kPairs = 128;  // tokens that are compared each with each
 
-// 2^d for -46 <= d <= 0, within a few units of 2^-53: 2^d = 2^n 2^f, |f| <= 1/2, and the Taylor series of e^(f ln 2)
-// to the 12th power (the next term is below 2^-52).
-__device__ __forceinline__ double exp2_f64(double d) {
-  const double n = __builtin_rint(d), t = (d - n) * 0.693147180559945309417;
-  double s = 1.0 / 479001600.0;
-  s = __builtin_fma(s, t, 1.0 / 39916800.0);
-  s = __builtin_fma(s, t, 1.0 / 3628800.0);
-  s = __builtin_fma(s, t, 1.0 / 362880.0);
-  s = __builtin_fma(s, t, 1.0 / 40320.0);
-  s = __builtin_fma(s, t, 1.0 / 5040.0);
-  s = __builtin_fma(s, t, 1.0 / 720.0);
-  s = __builtin_fma(s, t, 1.0 / 120.0);
-  s = __builtin_fma(s, t, 1.0 / 24.0);
-  s = __builtin_fma(s, t, 1.0 / 6.0);
-  s = __builtin_fma(s, t, 0.5);
-  s = __builtin_fma(s, t, 1.0);
-  s = __builtin_fma(s, t, 1.0);
-  return s * __hiloint2double((1023 + (int)n) << 20, 0);
-}
+// 2^(d + up) for -46 <= d <= 46, to within 2^-47: 2^d = 2^n 2^f, |f| <= 1/2, and the Taylor series of e^(f ln 2) to the
+// 11th power (the next term is below 2^-47).  The coefficients are held in scalar registers (as literals, each would be
+// moved to a register at every use).
+struct Exp2 {
+  double c[9];  // 1 / 11! ... 1 / 3!
+  __device__ __forceinline__ Exp2() {
+    double f = 1.0 / 39916800.0;
+#pragma unroll
+    for (int i = 0; i < 9; ++i) {
+      c[i] = f;
+      asm("" : "+s"(c[i]));
+      f *= 11 - i;
+    }
+  }
+  __device__ __forceinline__ double operator()(double d, int up = 0) const {
+    const double n = __builtin_rint(d), t = (d - n) * 0.693147180559945309417;
+    double s = c[0];
+#pragma unroll
+    for (int i = 1; i < 9; ++i) s = __builtin_fma(s, t, c[i]);
+    s = __builtin_fma(s, t, 0.5);
+    s = __builtin_fma(s, t, 1.0);
+    s = __builtin_fma(s, t, 1.0);
+    return __builtin_ldexp(s, (int)n + up);
+  }
+};
 
 // A row's settings.
 struct Settings {
@@ -68,16 +74,19 @@ struct Settings {
 };
 
 // Weight of logit x in a row (or chunk) whose largest is top.
-__device__ __forceinline__ double weight(float x, float top, double scale) {
+__device__ __forceinline__ double weight(const Exp2& exp2, float x, float top, double scale) {
   if (x == top) return top == -INFINITY ? 0.0 : 1.0;
   const double d = ((double)x - (double)top) * scale;
   if (!(d > -45.5)) return 0.0;
-  const double w = exp2_f64(d);
+  const double w = exp2(d);
   return w < 0x1p-45 ? 0.0 : w;
 }
-// ... as a multiple of 2^-44 (the mantissa bits of w 2^44 + 2^52).
-__device__ __forceinline__ uint64_t units(double w) {
-  return (uint64_t)__double_as_longlong(__builtin_fma(w, 0x1p44, 0x1p52)) & 0xfffffffffffffull;
+// ... as a multiple of 2^-44 (the mantissa bits of it + 2^52).  What lies below 2^-45.5 is rounded to zero.
+__device__ __forceinline__ uint64_t units_of(const Exp2& exp2, float x, float top, double scale) {
+  double d = ((double)x - (double)top) * scale;
+  if (top == INFINITY) d = x == INFINITY ? 0.0 : -46.0;
+  d = d >= -46.0 ? d : -46.0;  // (and where x is NaN)
+  return (uint64_t)__double_as_longlong(exp2(d, kSampleFrac) + 0x1p52) & 0xfffffffffffffull;
 }
 
 __device__ __forceinline__ uint64_t rank_of(float x, int i) {
@@ -178,6 +187,15 @@ struct RowReader {
                           : reinterpret_cast<const float*>(row)[i];
     return x != x ? -INFINITY : x;
   }
+  // The piece's bits, where it lies inside the row.
+  __device__ __forceinline__ bool inside(int g) const { return first(g) >= 0 && first(g) + n <= vocab; }
+  __device__ __forceinline__ u32x4 bits(int g) const {
+    return *reinterpret_cast<const u32x4*>(row + (int64_t)first(g) * (kBf16 ? 2 : 4));
+  }
+  __device__ __forceinline__ static float of_bits(const u32x4& v, int e) {  // as it is (NaN stays NaN)
+    if constexpr (kBf16) return __uint_as_float((e & 1) ? v[e / 2] & 0xffff0000u : v[e / 2] << 16);
+    else return __uint_as_float(v[e]);
+  }
   __device__ __forceinline__ void read(int g, float (&x)[n]) const {
     const int i0 = first(g);
     if (i0 >= 0 && i0 + n <= vocab) {
@@ -251,57 +269,82 @@ __device__ __forceinline__ uint64_t block_before(uint64_t x, uint64_t* sm, uint6
 }
 
 // What a chunk's sums of weights are multiplied by to be against the row's largest logit.
-__device__ __forceinline__ double rescaled(float c_top, float top, double scale) {
+__device__ __forceinline__ double rescaled(const Exp2& exp2, float c_top, float top, double scale) {
   if (c_top == top) return 1.0;
   const double d = ((double)c_top - (double)top) * scale;
-  return d > -46.0 ? exp2_f64(d) : d > -110.0 ? exp2_f64(d + 64.0) * 0x1p-64 : 0.0;
+  return d > -46.0 ? exp2(d) : d > -110.0 ? exp2(d + 64.0, -64) : 0.0;
 }
 __device__ __forceinline__ uint64_t scaled(uint64_t sum, double factor) {
   return factor == 1.0 ? sum : (uint64_t)((double)sum * factor);
 }
 
-template <bool kBf16, bool kDraw>
+template <bool kBf16>
 __global__ __launch_bounds__(kChunkThreads) void sample_chunk_kernel(SampleArgs a) {
   constexpr int n = RowReader<kBf16>::n, kMost = kRowThreads / kChunkThreads;  // pieces of a thread, at most
   constexpr int kWaves = kChunkThreads / kWave;
-  __shared__ unsigned long long sm_sum[kWaves][kSampleBins];
-  __shared__ uint32_t sm_cnt[kWaves][kSampleBins];
+  // Histograms, one for a wave: the sum of tokens' weights as multiples of 2^-40 below bit kCountAt, their number from
+  // there on.  (One for every eighth lane, where fewer lanes meet in a bin, took longer: the LDS leaves fewer workgroups
+  // to a CU.)
+  constexpr int kCountAt = 52;
+  static_assert(kMost * n * kWave <= 2048 && kSampleFrac - 4 + 11 < kCountAt, "sums and counts side by side");
+  __shared__ unsigned long long sm_hist[kWaves][kSampleBins];
+  __shared__ u32x4 sm_piece[kRowThreads];
   __shared__ uint64_t sm_red[kWaves];
-  __shared__ double sm_factor[kSampleMaxChunks];
-  __shared__ int sm_off[kSampleMaxChunks];
-  __shared__ int sm_int;
   const int chunk = blockIdx.x, r = blockIdx.y, tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
   const int b = r / a.rows_per_seq, t = r - b * a.rows_per_seq;
   if (a.n_query && t >= a.n_query[b]) return;
   const RowReader<kBf16> row(a, b, t);
   const Settings s(a, b);
-  float x[kMost][n];
-#pragma unroll
-  for (int j = 0; j < kMost; ++j) {
-    const int g = j * kChunkThreads + tid;
-#pragma unroll
-    for (int e = 0; e < n; ++e) x[j][e] = -INFINITY;
-    if (g < a.granules) row.read(chunk * a.granules + g, x[j]);
-  }
+  const Exp2 exp2;
   const bool filters = s.filters(), sums = !s.greedy && !s.counts_do();
   if (filters)
-    for (int i = lane; i < kSampleBins; i += kWave) {
-      sm_sum[wave][i] = 0;
-      sm_cnt[wave][i] = 0;
-    }
-  // the chunk's best token: its largest logit, then the lowest index that has it
-  float big = -INFINITY;
-#pragma unroll
-  for (int j = 0; j < kMost; ++j)
-#pragma unroll
-    for (int e = 0; e < n; ++e) big = fmaxf(big, x[j][e]);
+    for (int i = lane; i < kSampleBins; i += kWave) sm_hist[wave][i] = 0;
+  // the chunk's best token: its largest logit, then the lowest index that has it; the pieces wait in LDS
   uint64_t best = ~0ull;
-  if (big != -INFINITY) {
+  {
+    u32x4 v[kMost];
 #pragma unroll
-    for (int j = kMost - 1; j >= 0; --j)
+    for (int j = 0; j < kMost; ++j) {
+      const int g = chunk * a.granules + j * kChunkThreads + tid;
+      const bool is = j * kChunkThreads + tid < a.granules;
+      if (is && row.inside(g)) {
+        v[j] = row.bits(g);
+      } else {
 #pragma unroll
-      for (int e = n - 1; e >= 0; --e)
-        if (x[j][e] == big) best = rank_of(big, row.first(chunk * a.granules + j * kChunkThreads + tid) + e);
+        for (int e = 0; e < 4; ++e) v[j][e] = kBf16 ? 0xff80ff80u : 0xff800000u;
+        if (is)
+          for (int e = 0; e < n; ++e) {  // the row's ends
+            const int i = row.first(g) + e;
+            if (i < 0 || i >= a.vocab) continue;
+            const uint32_t y = __float_as_uint(row.at(i));
+            if constexpr (kBf16) {
+              const uint32_t keep = e & 1 ? 0xffffu : 0xffff0000u;
+#pragma unroll
+              for (int q = 0; q < 4; ++q)
+                if (e / 2 == q) v[j][q] = (v[j][q] & keep) | (e & 1 ? y : y >> 16);
+            } else {
+#pragma unroll
+              for (int q = 0; q < 4; ++q)
+                if (e == q) v[j][q] = y;
+            }
+          }
+      }
+    }
+    float big = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < kMost; ++j) {
+      sm_piece[j * kChunkThreads + tid] = v[j];
+#pragma unroll
+      for (int e = 0; e < n; ++e) big = fmaxf(big, row.of_bits(v[j], e));  // (fmaxf leaves NaN aside)
+    }
+    if (big != -INFINITY) {
+#pragma unroll
+      for (int j = kMost - 1; j >= 0; --j)
+#pragma unroll
+        for (int e = n - 1; e >= 0; --e)
+          if (row.of_bits(v[j], e) == big)
+            best = rank_of(big, row.first(chunk * a.granules + j * kChunkThreads + tid) + e);
+    }
   }
   best = wave_min(best);
   if (lane == 0) sm_red[wave] = best;
@@ -312,145 +355,45 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunk_kernel(SampleArgs 
   uint64_t sum = 0;
   if (!s.greedy && best != ~0ull) {
     const double oct = octave(top, s.scale);
-#pragma unroll
-    for (int j = 0; j < kMost; ++j)
+#pragma unroll 1
+    for (int j = 0; j < kMost; ++j) {
+      const u32x4 v = sm_piece[j * kChunkThreads + tid];
+      uint64_t w[n];
 #pragma unroll
       for (int e = 0; e < n; ++e) {
-        if (sums) {
-          const uint64_t w = units(weight(x[j][e], top, s.scale));
-          sum += w;
-          if (filters && w) {
-            const int bin = x[j][e] == top ? 0 : (int)(oct - octave(x[j][e], s.scale));
-            atomicAdd(&sm_sum[wave][bin], (unsigned long long)w);
-            atomicAdd(&sm_cnt[wave][bin], 1u);
-          }
-        } else if (x[j][e] != -INFINITY) {
-          const double d = x[j][e] == top ? 0.0 : oct - octave(x[j][e], s.scale);
-          if (d < kSampleBins - 2) atomicAdd(&sm_cnt[wave][(int)d], 1u);
-        }
+        w[e] = sums ? units_of(exp2, row.of_bits(v, e), top, s.scale) : 0;
+        sum += w[e];
       }
+      if (!filters) continue;
+#pragma unroll
+      for (int e = 0; e < n; ++e) {
+        const float x = row.of_bits(v, e);
+        const double d = x == top ? 0.0 : oct - octave(x, s.scale);
+        if (sums ? w[e] != 0 : d < kSampleBins - 2)  // (not for NaN)
+          atomicAdd(&sm_hist[wave][(int)d], ((w[e] + 8) >> 4) + (1ull << kCountAt));
+      }
+    }
   }
   sum = block_sum<kWaves>(sum, sm_red);
   const int64_t c0 = (int64_t)r * a.chunks, at = c0 + chunk;
   if (tid == 0) {
-    put(&a.c_top[at], top);
-    put(&a.c_best[at], best);
-    put(&a.c_sum[at], sum);
+    a.c_top[at] = top;
+    a.c_best[at] = best;
+    a.c_sum[at] = sum;
   }
-  if (filters && tid < kSampleBins) {
-    uint64_t h = 0;
-    uint32_t c = 0;
+  if (filters)
+    for (int i = tid; i < kSampleBins; i += kChunkThreads) {
+      uint64_t h = 0;
+      uint32_t c = 0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      h += sm_sum[w][tid];
-      c += sm_cnt[w][tid];
-    }
-    if (sums) put(&a.h_sum[at * kSampleBins + tid], h);
-    put(&a.h_cnt[at * kSampleBins + tid], c);
-  }
-  if (!arrive_last(&a.arrived[r], a.chunks, &sm_int)) return;
-
-  // ---- the last workgroup of a row joins the chunks and plans the rest
-  uint64_t row_best = ~0ull;
-  for (int c = tid; c < a.chunks; c += kChunkThreads) {
-    const uint64_t y = get(&a.c_best[c0 + c]);
-    row_best = y < row_best ? y : row_best;
-  }
-  row_best = wave_min(row_best);
-  __syncthreads();
-  if (lane == 0) sm_red[wave] = row_best;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) row_best = sm_red[w] < row_best ? sm_red[w] : row_best;
-  const bool none = row_best == ~0ull;
-  const float row_top = none ? -INFINITY : logit_of_rank(row_best);
-  SamplePlan plan{};
-  if (none || s.greedy) {  // nothing to draw from, or nothing to draw
-    if (tid == 0) {
-      a.plan[r] = plan;
-      a.row[r] = {none ? 0 : row_best, none ? 0 : 1ull << kSampleFrac, row_top};
-      if constexpr (kDraw) a.token[b] = none ? -1 : (int)(row_best & (kSampleMaxVocab - 1));
-    }
-    return;
-  }
-  const double oct = octave(row_top, s.scale);
-  uint64_t all_sum = 0;
-  for (int c = tid; c < a.chunks; c += kChunkThreads) {
-    const float c_top = get(&a.c_top[c0 + c]);
-    const double off = c_top == row_top ? 0.0 : oct - octave(c_top, s.scale);
-    sm_off[c] = off < kSampleBins ? (int)off : kSampleBins;
-    sm_factor[c] = rescaled(c_top, row_top, s.scale);
-    if (sums) all_sum += scaled(get(&a.c_sum[c0 + c]), sm_factor[c]);
-  }
-  if (!filters) {
-    all_sum = block_sum<kWaves>(all_sum, sm_red);
-    plan.mode = kDraw ? kRowWhole : kRowDone;
-    plan.all_sum = all_sum;
-    if (tid == 0) {
-      a.plan[r] = plan;
-      a.row[r] = {~0ull, all_sum, row_top};
-    }
-    return;
-  }
-  __syncthreads();
-  uint64_t my_cnt = 0, my_sum = 0;
-  if (tid < kSampleBins) {
-#pragma unroll 8
-    for (int c = 0; c < a.chunks; ++c) {
-      const int bin = tid - sm_off[c];
-      const int64_t h = (c0 + c) * kSampleBins + (bin < 0 ? 0 : bin);
-      const uint32_t y = get(&a.h_cnt[h]);
-      my_cnt += bin < 0 ? 0 : y;
-      if (sums) {
-        const uint64_t z = get(&a.h_sum[h]);
-        my_sum += bin < 0 ? 0 : scaled(z, sm_factor[c]);
+      for (int w = 0; w < kWaves; ++w) {
+        h += sm_hist[w][i] & ((1ull << kCountAt) - 1);
+        c += (uint32_t)(sm_hist[w][i] >> kCountAt);
       }
+      h <<= 4;
+      if (sums) a.h_sum[at * kSampleBins + i] = h;
+      a.h_cnt[at * kSampleBins + i] = c;
     }
-  }
-  uint64_t all_cnt;
-  const uint64_t cnt_before = block_before<kWaves>(my_cnt, sm_red, all_cnt);
-  const uint64_t sum_before = block_before<kWaves>(my_sum, sm_red, all_sum);
-  // the eighth of an octave in which the kept set ends, by count or sum, and by min_p
-  const bool by_count = s.k > 0 && (uint64_t)s.k < all_cnt;
-  double target = by_count ? (double)s.k : s.p * (double)all_sum;
-  if (!by_count && s.counts_do()) target = (double)all_cnt;  // (fewer tokens than top_k: they are few)
-  const bool count_scale = by_count || s.counts_do();
-  __syncthreads();
-  if (tid == 0) sm_int = kSampleBins - 1;
-  __syncthreads();
-  if (tid < kSampleBins && my_cnt &&
-      (count_scale ? (double)(cnt_before + my_cnt) : (double)(sum_before + my_sum)) >= target)
-    atomicMin(&sm_int, tid);
-  __syncthreads();
-  int bin = sm_int;
-  plan.least = ~0ull;
-  if (s.m > 0.0) {
-    const float m = (float)s.m;
-    plan.least = whole_key(least_key(row_top, (double)row_top + (double)__log2f(m) / s.scale,
-                                     [&](float x) { return weight(x, row_top, s.scale) >= s.m; }));
-    const float x = logit_of_rank(plan.least);
-    const int bin_m = x == row_top ? 0 : (int)(oct - octave(x, s.scale));
-    if (bin_m < bin) {
-      bin = bin_m;
-      target = -1.0;
-    }
-  }
-  if (tid == bin) {  // (a eighth of an octave that only min_p names may hold no token)
-    const uint64_t upto = cnt_before + my_cnt;
-    const bool p_of_k = by_count && s.p < 1.0;  // top_p of a sum that the top_k leave
-    plan.mode = upto <= kFew || s.counts_do() ? kRowFew : my_cnt <= kList && !p_of_k ? kRowList : kRowRead;
-    plan.bin = bin;
-    plan.hi = whole_key(bin_key(row_top, s.scale, bin));
-    plan.lo = plan.mode == kRowList && bin > 0 ? whole_key(bin_key(row_top, s.scale, bin - 1)) + 1 : 0;
-    plan.before_cnt = cnt_before;
-    plan.before_sum = sum_before;
-    plan.all_sum = all_sum;
-    plan.target = target;
-    plan.by_count = by_count;
-    if (plan.mode == kRowFew && upto > kFew) plan.mode = kRowRead;
-    a.plan[r] = plan;
-    a.row[r] = {0, 0, row_top};
-  }
 }
 
 // Of the tokens of a chunk (one piece to a thread) with rank at most `last`, the one at which the running sum of
@@ -459,30 +402,27 @@ template <bool kBf16, class Value>
 __device__ int draw_in_chunk(const SampleArgs& a, const RowReader<kBf16>& row, int chunk, uint64_t target, Value value,
                              uint64_t* sm, int* sm_token) {
   constexpr int n = RowReader<kBf16>::n;
-  uint64_t v[n], own = 0;
-  int i0 = 0;
-#pragma unroll
-  for (int e = 0; e < n; ++e) v[e] = 0;
-  if ((int)threadIdx.x < a.granules) {
-    const int g = chunk * a.granules + threadIdx.x;
-    float x[n];
-    row.read(g, x);
-    i0 = row.first(g);
-#pragma unroll
-    for (int e = 0; e < n; ++e) {
-      v[e] = x[e] == -INFINITY ? 0 : value(x[e], i0 + e);
-      own += v[e];
-    }
-  }
+  const int i0 = row.first(chunk * a.granules + (int)threadIdx.x);
+  auto at = [&](int i) -> uint64_t {
+    if (i < 0 || i >= a.vocab) return 0;
+    const float x = row.at(i);
+    return x == -INFINITY ? 0 : value(x, i);
+  };
+  uint64_t own = 0;
+  if ((int)threadIdx.x < a.granules)
+#pragma unroll 1
+    for (int e = 0; e < n; ++e) own += at(i0 + e);
   if (threadIdx.x == 0) *sm_token = -1;
   uint64_t all;
   uint64_t run = block_before<kRowWaves>(own, sm, all);
   if (all && target >= all) target = all - 1;
-#pragma unroll
-  for (int e = 0; e < n; ++e) {
-    if (run <= target && target < run + v[e]) *sm_token = i0 + e;
-    run += v[e];
-  }
+  if (run <= target && target < run + own)  // one thread's tokens
+#pragma unroll 1
+    for (int e = 0; e < n; ++e) {
+      const uint64_t v = at(i0 + e);
+      if (run <= target && target < run + v) *sm_token = i0 + e;
+      run += v;
+    }
   __syncthreads();
   return *sm_token;
 }
@@ -522,57 +462,175 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
   const int r = blockIdx.y, tid = threadIdx.x;
   const int b = r / a.rows_per_seq, t = r - b * a.rows_per_seq;
   if (a.n_query && t >= a.n_query[b]) return;
-  const SamplePlan plan = a.plan[r];
-  const bool lists = plan.mode == kRowFew || plan.mode == kRowList;
-  if (plan.mode == kRowDone || (!lists && blockIdx.x > 0)) return;
-  const float top = a.row[r].top;
   const RowReader<kBf16> row(a, b, t);
   const Settings s(a, b);
+  const Exp2 exp2;
   const int64_t c0 = (int64_t)r * a.chunks;
   const int pieces = a.granules * a.chunks;
-  auto units_of = [&](float x) { return units(weight(x, top, s.scale)); };
+  const bool filters = s.filters(), sums = !s.greedy && !s.counts_do();
+
+  // ---- the chunks joined: the row's best token, the sum of its weights, its histogram
+  uint64_t best = tid < a.chunks ? a.c_best[c0 + tid] : ~0ull;
+  const float c_top = tid < a.chunks ? a.c_top[c0 + tid] : -INFINITY;
+  const uint64_t c_sum = sums && tid < a.chunks ? a.c_sum[c0 + tid] : 0;
+  best = wave_min(best);
+  if ((tid & (kWave - 1)) == 0) sm_red[tid / kWave] = best;
+  sm_sum[tid] = 0;
+  sm_cnt[tid] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kRowWaves; ++w) best = sm_red[w] < best ? sm_red[w] : best;
+  const bool none = best == ~0ull;
+  const float top = none ? -INFINITY : logit_of_rank(best);
+  if (none || s.greedy) {  // nothing to draw from, or nothing to draw
+    if (tid == 0 && blockIdx.x == 0) {
+      a.row[r] = {none ? 0 : best, none ? 0 : 1ull << kSampleFrac, top};
+      if constexpr (kDraw) a.token[b] = none ? -1 : (int)(best & (kSampleMaxVocab - 1));
+    }
+    return;
+  }
+  const double oct = octave(top, s.scale);
+  uint64_t all_sum = 0;
+  if (tid < a.chunks) {
+    const double off = c_top == top ? 0.0 : oct - octave(c_top, s.scale);
+    const double factor = rescaled(exp2, c_top, top, s.scale);
+    sm_off[tid] = off < kSampleBins ? (int)off : kSampleBins;
+    sm_factor[tid] = factor;
+    all_sum = scaled(c_sum, factor);
+    sm_chunk_sum[tid] = all_sum;
+  }
+  SamplePlan plan{};
+  plan.mode = kRowWhole;
+  plan.least = ~0ull;
+  if (!filters) {
+    if (blockIdx.x > 0) return;
+    if constexpr (!kDraw) {
+      all_sum = block_sum<kRowWaves>(all_sum, sm_red);
+      if (tid == 0) a.row[r] = {~0ull, all_sum, top};
+      return;
+    }
+    __syncthreads();
+  } else {
+    __syncthreads();
+#pragma unroll 4
+    for (int e = tid; e < a.chunks * kSampleBins; e += kRowThreads) {
+      const int c = e / kSampleBins, to = e - c * kSampleBins + sm_off[c];
+      const uint32_t y = a.h_cnt[c0 * kSampleBins + e];
+      const uint64_t z = sums ? a.h_sum[c0 * kSampleBins + e] : 0;
+      if (to >= kSampleBins || !y) continue;
+      atomicAdd(&sm_cnt[to], y);
+      if (sums) atomicAdd(&sm_sum[to], (unsigned long long)scaled(z, sm_factor[c]));
+    }
+    __syncthreads();
+    const uint64_t my_cnt = tid < kSampleBins ? sm_cnt[tid] : 0, my_sum = tid < kSampleBins ? sm_sum[tid] : 0;
+    uint64_t all_cnt;
+    const uint64_t cnt_before = block_before<kRowWaves>(my_cnt, sm_red, all_cnt);
+    const uint64_t sum_before = block_before<kRowWaves>(my_sum, sm_red, all_sum);
+    // the eighth of an octave in which the kept set ends, by count or sum, and by min_p
+    const bool by_count = s.k > 0 && (uint64_t)s.k < all_cnt;
+    const bool count_scale = by_count || s.counts_do();
+    double target = by_count ? (double)s.k : s.counts_do() ? (double)all_cnt : s.p * (double)all_sum;
+    if (tid == 0) sm_int[0] = kSampleBins - 1;
+    __syncthreads();
+    if (my_cnt && (count_scale ? (double)(cnt_before + my_cnt) : (double)(sum_before + my_sum)) >= target)
+      atomicMin(&sm_int[0], tid);
+    __syncthreads();
+    int bin = sm_int[0];
+    if (s.m > 0.0) {
+      plan.least = whole_key(least_key(top, (double)top + (double)__log2f((float)s.m) / s.scale,
+                                       [&](float x) { return weight(exp2, x, top, s.scale) >= s.m; }));
+      const float x = logit_of_rank(plan.least);
+      const int bin_m = x == top ? 0 : (int)(oct - octave(x, s.scale));
+      if (bin_m < bin) {
+        bin = bin_m;
+        target = -1.0;
+      }
+    }
+    if (tid == bin) {  // (one that only min_p names may hold no token)
+      sm_u64[0] = cnt_before;
+      sm_u64[1] = sum_before;
+      sm_u64[2] = my_cnt;
+    }
+    __syncthreads();
+    const uint64_t in = sm_u64[2];
+    const bool p_of_k = by_count && s.p < 1.0;  // top_p of a sum that the top_k leave
+    plan.mode = sm_u64[0] + in <= kFew ? kRowFew : in <= kList && !p_of_k && !s.counts_do() ? kRowList : kRowRead;
+    plan.bin = bin;
+    plan.hi = whole_key(bin_key(top, s.scale, bin));
+    plan.lo = plan.mode == kRowList && bin > 0 ? whole_key(bin_key(top, s.scale, bin - 1)) + 1 : 0;
+    plan.before_cnt = plan.mode == kRowList ? sm_u64[0] : 0;
+    plan.before_sum = plan.mode == kRowList ? sm_u64[1] : 0;
+    plan.all_sum = all_sum;
+    plan.target = target;
+    plan.by_count = by_count;
+    __syncthreads();
+  }
+  const bool lists = plan.mode == kRowFew || plan.mode == kRowList;
+  if (!lists && blockIdx.x > 0) return;
   // calls f(rank, units) for every token of pieces [g0, g1) that has any and whose rank lies in [lo, hi]
   auto each = [&](int g0, int g1, uint64_t lo, uint64_t hi, auto f) {
     const float x_hi = ceiling_of(lo), x_lo = bottom_of(hi);
+#pragma unroll 4
     for (int g = g0 + tid; g < g1; g += kRowThreads) {
-      float x[n];
-      row.read(g, x);
-      bool any = false;
+      uint32_t hits = 0;
+      if (row.inside(g)) {
+        const u32x4 v = row.bits(g);
 #pragma unroll
-      for (int e = 0; e < n; ++e) any |= x[e] >= x_lo && x[e] <= x_hi;
-      if (!any) continue;
-#pragma unroll
-      for (int e = 0; e < n; ++e)
-        if (x[e] >= x_lo && x[e] <= x_hi && x[e] != -INFINITY) {
-          const uint64_t c = rank_of(x[e], row.first(g) + e);
-          const uint64_t w = c >= lo && c <= hi ? units_of(x[e]) : 0;
-          if (w) f(c, w);
+        for (int e = 0; e < n; ++e) {
+          const float x = row.of_bits(v, e);
+          hits |= x >= x_lo && x <= x_hi ? 1u << e : 0u;
         }
+      } else {
+        const int i0 = row.first(g);
+        for (int e = 0; e < n; ++e) hits |= i0 + e >= 0 && i0 + e < a.vocab ? 1u << e : 0u;
+      }
+      while (hits) {
+        const int i = row.first(g) + __builtin_ctz(hits);
+        hits &= hits - 1;
+        const float x = row.at(i);
+        const uint64_t c = rank_of(x, i);
+        const uint64_t w = x != -INFINITY && c >= lo && c <= hi ? units_of(exp2, x, top, s.scale) : 0;
+        if (w) f(c, w);
+      }
     }
   };
   int m = 0;  // tokens in the list
   if (lists) {
     const int share = (pieces + a.parts - 1) / a.parts;
     uint64_t* list = a.list + (int64_t)r * kList * 2;
+    if (tid == 0) sm_cnt[0] = 0;
+    __syncthreads();
     each(blockIdx.x * share, min(pieces, (int)(blockIdx.x + 1) * share), plan.lo, plan.hi, [&](uint64_t c, uint64_t w) {
-      const uint32_t at = __hip_atomic_fetch_add(&a.listed[r], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      const uint32_t at = atomicAdd(&sm_cnt[0], 1u);
       if (at < kList) {
-        put(list + 2 * at, c);
-        put(list + 2 * at + 1, w);
+        sm_rank[at] = c;
+        sm_w[at] = w;
       }
     });
-    if (!arrive_last(&a.arrived[r], a.parts, &sm_int[0])) return;
-    m = min((int)get(&a.listed[r]), kList);
-    for (int j = tid; j < m; j += kRowThreads) {
-      sm_rank[j] = get(list + 2 * j);
-      sm_w[j] = get(list + 2 * j + 1);
-    }
     __syncthreads();
-    if (tid == 0) put(&a.listed[r], 0u);
+    m = min((int)sm_cnt[0], kList);
+    if (a.parts > 1) {
+      if (tid == 0) sm_cnt[1] = m ? __hip_atomic_fetch_add(&a.listed[r], (uint32_t)m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
+      __syncthreads();
+      const int base = (int)sm_cnt[1];
+      for (int j = tid; j < m && base + j < kList; j += kRowThreads) {
+        put(list + 2 * (base + j), sm_rank[j]);
+        put(list + 2 * (base + j) + 1, sm_w[j]);
+      }
+    }
+    if (!arrive_last(&a.arrived[r], a.parts, &sm_int[0])) return;
+    if (a.parts > 1) {
+      m = min((int)get(&a.listed[r]), kList);
+      for (int j = tid; j < m; j += kRowThreads) {
+        sm_rank[j] = get(list + 2 * j);
+        sm_w[j] = get(list + 2 * j + 1);
+      }
+      __syncthreads();
+      if (tid == 0) put(&a.listed[r], 0u);
+    }
   }
-  if (plan.mode == kRowFew) {
+  if (plan.mode == kRowFew && m <= kPairs) {
     // ---- few: each compared with each
-    m = min(m, kFew);
     int share = 64;  // threads to a token
     while (share * m > kRowThreads) share >>= 1;
     const int e = tid / share, part = tid % share;
@@ -593,7 +651,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
     // (without a top_k the list need not hold all that the sum is over)
     const uint64_t z_k = s.counts_do() || plan.by_count ? block_sum<kRowWaves>(kept && part == 0 ? w : 0, sm_red) : plan.all_sum;
     if (s.p < 1.0) kept &= place == 0 || (double)before < s.p * (double)z_k;
-    kept &= place == 0 || weight(logit_of_rank(c), top, s.scale) >= s.m;
+    kept &= place == 0 || weight(exp2, logit_of_rank(c), top, s.scale) >= s.m;
     const uint64_t z = block_sum<kRowWaves>(kept && part == 0 ? w : 0, sm_red);
     if (tid == 0) sm_u64[3] = 0;
     __syncthreads();
@@ -620,7 +678,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
   // ---- many: the last token by ever finer ranges of ranks
   uint64_t last = ~0ull;  // its rank
   auto each_token = [&](uint64_t lo, uint64_t hi, auto f) {
-    if (plan.mode == kRowList) {
+    if (lists) {
       for (int j = tid; j < m; j += kRowThreads)
         if (sm_rank[j] >= lo && sm_rank[j] <= hi) f(sm_rank[j], sm_w[j]);
     } else {
@@ -629,9 +687,33 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
   };
   // the first token of ranks lo .. hi at which the running count (or sum), from what is before them, reaches the
   // target, else the last there is; the sum up to it
+  constexpr int kCompare = 32;
   auto find_token = [&](uint64_t lo, uint64_t hi, uint64_t cnt_b, uint64_t sum_b, bool by_sum, double target,
                         uint64_t& sum) {
     for (;;) {
+      // the ranks that there are
+      __syncthreads();
+      if (tid == 0) {
+        sm_u64[0] = ~0ull;
+        sm_u64[1] = 0;
+      }
+      __syncthreads();
+      if (lists) {
+        uint64_t least = ~0ull, most = 0;
+        each_token(lo, hi, [&](uint64_t c, uint64_t) {
+          least = c < least ? c : least;
+          most = c > most ? c : most;
+        });
+        least = wave_min(least);
+        most = ~wave_min(~most);
+        if ((tid & (kWave - 1)) == 0 && most >= least) {
+          atomicMin(reinterpret_cast<unsigned long long*>(&sm_u64[0]), (unsigned long long)least);
+          atomicMax(reinterpret_cast<unsigned long long*>(&sm_u64[1]), (unsigned long long)most);
+        }
+        __syncthreads();
+        lo = sm_u64[0];
+        hi = sm_u64[1];
+      }
       const int bits = hi == lo ? 0 : 64 - __clzll((long long)(hi - lo));
       const int shift = bits > 10 ? bits - 10 : 0;
       __syncthreads();
@@ -662,6 +744,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
         sm_u64[2] = sb + os;
       }
       __syncthreads();
+      const uint32_t in = sm_cnt[j];
       cnt_b = sm_u64[0];
       sum_b = sm_u64[1];
       sum = sm_u64[2];
@@ -669,42 +752,131 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
       if (shift == 0) return lo;
       const uint64_t end = lo + ((1ull << shift) - 1);
       hi = end < hi ? end : hi;
+      if (in > kCompare) continue;
+      // few: each compared with each, in the histogram's place
+      __syncthreads();
+      if (tid == 0) {
+        sm_int[0] = 0;
+        sm_u64[0] = ~0ull;
+        sm_u64[1] = sum;
+      }
+      __syncthreads();
+      each_token(lo, hi, [&](uint64_t c, uint64_t w) {
+        const int at = atomicAdd(&sm_int[0], 1);
+        sm_sum[at] = c;
+        sm_sum[kCompare + at] = w;
+      });
+      __syncthreads();
+      const int all = sm_int[0];
+      if (tid < all) {
+        const uint64_t c = sm_sum[tid], w = sm_sum[kCompare + tid];
+        uint64_t cb2 = cnt_b + 1, sb2 = sum_b + w;
+        uint64_t worse = 0;
+        for (int i = 0; i < all; ++i) {
+          const bool better = sm_sum[i] < c;
+          cb2 += better;
+          sb2 += better ? sm_sum[kCompare + i] : 0;
+          worse += sm_sum[i] > c;
+        }
+        const bool reached = (by_sum ? (double)sb2 : (double)cb2) >= target || !worse;
+        if (reached) atomicMin(reinterpret_cast<unsigned long long*>(&sm_u64[0]), (unsigned long long)c);
+      }
+      __syncthreads();
+      const uint64_t found = sm_u64[0];
+      if (tid < all && sm_sum[tid] == found) {
+        uint64_t sb2 = sum_b;
+        for (int i = 0; i < all; ++i) sb2 += sm_sum[i] <= found ? sm_sum[kCompare + i] : 0;
+        sm_u64[1] = sb2;
+      }
+      __syncthreads();
+      sum = sm_u64[1];
+      return found;
     }
   };
-  uint64_t sum;
-  if (plan.mode == kRowList) {
-    last = plan.target < 0.0 ? plan.least
-                             : find_token(plan.lo, plan.hi, plan.before_cnt, plan.before_sum, !plan.by_count, plan.target, sum);
-  } else if (plan.mode == kRowRead) {
-    // no more than 2^-45.5 of the largest weight: every token that has any
-    const uint64_t end = whole_key(bin_key(top, s.scale, kSampleBins - 1));
-    uint64_t z = s.counts_do() ? 0 : plan.all_sum;
-    if (s.k > 0) last = find_token(0, end, 0, 0, false, (double)s.k, z);
-    if (s.p < 1.0) {
-      const uint64_t at = find_token(0, end, 0, 0, true, s.p * (double)z, sum);
+  if (plan.mode != kRowWhole && !(plan.mode == kRowList && plan.target < 0.0)) {
+    uint64_t z = plan.all_sum;  // the sum that top_p is a part of
+    if (!plan.by_count && s.counts_do()) {  // fewer tokens than top_k: the list's
+      uint64_t w = 0;
+      for (int j = tid; j < m; j += kRowThreads) w += sm_w[j];
+      z = block_sum<kRowWaves>(w, sm_red);
+    }
+    // all tokens whose weight is no less than 2^-45.5 of the largest
+    const uint64_t end = lists ? plan.hi : whole_key(bin_key(top, s.scale, kSampleBins - 1));
+#pragma unroll 1
+    for (int by_sum = 0; by_sum < 2; ++by_sum) {  // the last of the top_k, then the last that top_p keeps
+      if (by_sum ? !(s.p < 1.0) || plan.target < 0.0 : !plan.by_count) continue;
+      uint64_t sum;
+      const uint64_t at = find_token(lists ? plan.lo : 0, end, plan.before_cnt, plan.before_sum, by_sum,
+                                     by_sum ? s.p * (double)z : (double)s.k, sum);
       last = at < last ? at : last;
+      if (!by_sum) z = sum;
     }
   }
   if (plan.mode != kRowWhole && plan.least < last) last = plan.least;
 
+  if (plan.mode == kRowFew) {
+    // ---- the kept tokens are in the list: the draw by the upper and then the lower bits of their index
+    constexpr int kLow = kSampleIdxBits - 10;
+    uint64_t z = 0, run = 0, target = 0;
+    int high = 0;
+#pragma unroll
+    for (int level = 0; level < 2; ++level) {
+      __syncthreads();
+      sm_sum[tid] = 0;
+      __syncthreads();
+      for (int j = tid; j < m; j += kRowThreads) {
+        const int i = (int)sm_rank[j] & (kSampleMaxVocab - 1);
+        if (sm_rank[j] <= last && (level == 0 || i >> kLow == high))
+          atomicAdd(&sm_sum[level == 0 ? i >> kLow : i & ((1 << kLow) - 1)], (unsigned long long)sm_w[j]);
+      }
+      __syncthreads();
+      const uint64_t w = sm_sum[tid];
+      uint64_t all;
+      const uint64_t before = run + block_before<kRowWaves>(w, sm_red, all);
+      if (level == 0) {
+        z = all;
+        float u = kDraw ? a.u[b] : 0.f;
+        u = u > 0.f ? u : 0.f;
+        target = (uint64_t)((double)u * (double)z);
+        if (target >= z) target = z - 1;
+        if (tid == 0) a.row[r] = {last, z, top};
+        if constexpr (!kDraw) return;
+      }
+      if (before <= target && target < before + w) {
+        if (level == 0) {
+          sm_int[0] = tid;
+          sm_u64[0] = before;
+        } else {
+          a.token[b] = (high << kLow) + tid;
+        }
+      }
+      __syncthreads();
+      if (level == 0) {
+        high = sm_int[0];
+        run = sm_u64[0];
+      }
+    }
+    return;
+  }
+
   // ---- sums of the kept weights by chunks
   __syncthreads();
-  for (int c = tid; c < a.chunks; c += kRowThreads) {
-    const float c_top = a.c_top[c0 + c];
-    const double off = c_top == top ? 0.0 : octave(top, s.scale) - octave(c_top, s.scale);
-    sm_off[c] = off < kSampleBins ? (int)off : kSampleBins;
-    sm_factor[c] = rescaled(c_top, top, s.scale);
-    sm_chunk_sum[c] = plan.mode == kRowWhole ? scaled(a.c_sum[c0 + c], sm_factor[c]) : 0;
-  }
+  if (plan.mode != kRowWhole && tid < a.chunks) sm_chunk_sum[tid] = 0;
   __syncthreads();
   const int chunk_bits = 31 - __clz(a.granules * n);
-  if (plan.mode == kRowList)
-    for (int e = tid; e < a.chunks * kSampleBins; e += kRowThreads) {
-      const int c = e / kSampleBins, bin = e - c * kSampleBins;
-      if (sm_off[c] + bin >= plan.bin) continue;
-      const uint64_t x = a.h_sum[c0 * kSampleBins + e];
-      if (x) atomicAdd(&sm_chunk_sum[c], (unsigned long long)scaled(x, sm_factor[c]));
+  if (plan.mode == kRowList) {  // (a list with all that may be kept returned above)
+    for (int c = tid / kWave; c < a.chunks; c += kRowWaves) {
+      uint64_t x = 0;
+#pragma unroll
+      for (int bin = tid & (kWave - 1); bin < kSampleBins; bin += kWave) {
+        const uint64_t y = a.h_sum[(c0 + c) * kSampleBins + bin];
+        x += sm_off[c] + bin < plan.bin ? scaled(y, sm_factor[c]) : 0;
+      }
+      x = wave_sum(x);
+      if ((tid & (kWave - 1)) == 0) sm_chunk_sum[c] = x;
     }
+    __syncthreads();
+  }
   if (plan.mode != kRowWhole)
     each_token(0, last, [&](uint64_t c, uint64_t w) {
       const uint32_t i = (uint32_t)c & (kSampleMaxVocab - 1);
@@ -718,7 +890,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
   if constexpr (kDraw) {
     if (chunk < 0) return;
     const int token = draw_in_chunk<kBf16>(
-        a, row, chunk, sm_u64[0], [&](float x, int i) { return rank_of(x, i) <= last ? units_of(x) : 0; }, sm_red,
+        a, row, chunk, sm_u64[0], [&](float x, int i) { return rank_of(x, i) <= last ? units_of(exp2, x, top, s.scale) : 0; }, sm_red,
         &sm_int[1]);
     if (tid == 0) a.token[b] = token;
   }
@@ -732,11 +904,12 @@ __global__ __launch_bounds__(kChunkThreads) void sample_probs_kernel(SampleArgs 
   if (i >= a.vocab) return;
   const RowReader<kBf16> row(a, b, 0);
   const Settings s(a, b);
+  const Exp2 exp2;
   const SampleRow o = a.row[b];
   const float x = row.at(i);
   double p = 0.0;
   if (o.sum && x != -INFINITY && rank_of(x, i) <= o.last)
-    p = weight(x, o.top, s.scale) / ((double)o.sum * 0x1p-44);
+    p = weight(exp2, x, o.top, s.scale) / ((double)o.sum * 0x1p-44);
   a.probs[b * a.probs_sb + i] = (float)p;
 }
 
@@ -750,6 +923,7 @@ __global__ __launch_bounds__(kRowThreads) void verify_rest_kernel(SampleArgs a) 
   const int chunk = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
   const int T = a.n_query ? clampi(a.n_query[b], 0, a.rows_per_seq) : a.rows_per_seq;
   const Settings s(a, b);
+  const Exp2 exp2;
   if (T == 0) {
     if (chunk == 0 && tid == 0) {
       a.accepted[b] = 0;
@@ -765,7 +939,7 @@ __global__ __launch_bounds__(kRowThreads) void verify_rest_kernel(SampleArgs a) 
       const SampleRow o = a.row[b * a.rows_per_seq + tid];
       if (x >= 0 && x < a.vocab && o.sum) {
         const float l = RowReader<kBf16>(a, b, tid).at(x);
-        const double p = l != -INFINITY && rank_of(l, x) <= o.last ? weight(l, o.top, s.scale) / ((double)o.sum * 0x1p-44) : 0.0;
+        const double p = l != -INFINITY && rank_of(l, x) <= o.last ? weight(exp2, l, o.top, s.scale) / ((double)o.sum * 0x1p-44) : 0.0;
         const double q = a.q ? (double)a.q[b * a.q_sb + tid * a.q_st + x] : 1.0;
         ok = (double)a.u_accept[b * a.ua_sb + tid] * q < p;
       }
@@ -783,7 +957,7 @@ __global__ __launch_bounds__(kRowThreads) void verify_rest_kernel(SampleArgs a) 
   const double z = (double)o.sum * 0x1p-44;
   // probabilities as multiples of 2^-60
   auto whole = [&](float x, int i) -> double {
-    return rank_of(x, i) <= o.last ? weight(x, o.top, s.scale) / z : 0.0;
+    return rank_of(x, i) <= o.last ? weight(exp2, x, o.top, s.scale) / z : 0.0;
   };
   auto rest = [&](double p, int i) {
     if (rejected) p -= q ? (double)q[i] : i == x_draft ? 1.0 : 0.0;
@@ -792,14 +966,15 @@ __global__ __launch_bounds__(kRowThreads) void verify_rest_kernel(SampleArgs a) 
   auto fixed = [](double p) { return (uint64_t)__builtin_rint(p * 0x1p60); };
   uint64_t r_sum = 0, p_sum = 0;
   if (o.sum && tid < a.granules) {
-    const int g = chunk * a.granules + tid;
-    float x[n];
-    row.read(g, x);
-#pragma unroll
+    const int i0 = row.first(chunk * a.granules + tid);
+    const float x_lo = bottom_of(o.last);
+#pragma unroll 1
     for (int e = 0; e < n; ++e) {
-      const int i = row.first(g) + e;
-      if (x[e] == -INFINITY) continue;
-      const double p = whole(x[e], i);
+      const int i = i0 + e;
+      if (i < 0 || i >= a.vocab) continue;
+      const float x = row.at(i);
+      if (x < x_lo || x == -INFINITY) continue;
+      const double p = whole(x, i);
       if (p > 0.0) {
         p_sum += fixed(p);
         r_sum += fixed(rest(p, i));
@@ -836,7 +1011,7 @@ __global__ __launch_bounds__(kRowThreads) void verify_rest_kernel(SampleArgs a) 
 
 template <bool kBf16>
 hipError_t launch_sample_of(const SampleArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL((sample_chunk_kernel<kBf16, true>), dim3(a.chunks, a.batch), dim3(kChunkThreads), 0, stream, a);
+  hipLaunchKernelGGL((sample_chunk_kernel<kBf16>), dim3(a.chunks, a.batch), dim3(kChunkThreads), 0, stream, a);
   hipLaunchKernelGGL((sample_row_kernel<kBf16, true>), dim3(a.parts, a.batch), dim3(kRowThreads), 0, stream, a);
   if (a.probs)
     hipLaunchKernelGGL((sample_probs_kernel<kBf16>), dim3((a.vocab + kChunkThreads - 1) / kChunkThreads, a.batch),
@@ -847,7 +1022,7 @@ hipError_t launch_sample_of(const SampleArgs& a, hipStream_t stream) {
 template <bool kBf16>
 hipError_t launch_verify_of(const SampleArgs& a, hipStream_t stream) {
   const int rows = a.batch * a.rows_per_seq;
-  hipLaunchKernelGGL((sample_chunk_kernel<kBf16, false>), dim3(a.chunks, rows), dim3(kChunkThreads), 0, stream, a);
+  hipLaunchKernelGGL((sample_chunk_kernel<kBf16>), dim3(a.chunks, rows), dim3(kChunkThreads), 0, stream, a);
   hipLaunchKernelGGL((sample_row_kernel<kBf16, false>), dim3(a.parts, rows), dim3(kRowThreads), 0, stream, a);
   hipLaunchKernelGGL((verify_rest_kernel<kBf16>), dim3(a.chunks, a.batch), dim3(kRowThreads), 0, stream, a);
   return hipGetLastError();

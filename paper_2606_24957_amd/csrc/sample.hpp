@@ -18,7 +18,7 @@ constexpr int kSampleBins = 368;     // eighths of octaves from the largest weig
 constexpr int kSampleFew = 1024;     // tokens ranked by comparing each with each
 constexpr int kSampleList = 4096;    // tokens of a list
 constexpr int kSampleMaxWindow = 64; // tokens of a verification window
-constexpr int kSampleMaxChunks = 264;  // 2^18 fp32 logits in chunks of 256 pieces, wherever the row begins
+constexpr int kSampleMaxChunks = 136;  // 2^18 fp32 logits in chunks of 512 pieces, wherever the row begins
 
 struct SampleRow {  // what is known of a row once its filters are resolved
   uint64_t last;    // rank of the last kept token (0: none is)
@@ -28,7 +28,6 @@ struct SampleRow {  // what is known of a row once its filters are resolved
 
 // How the rest of a row is done, from its histogram.
 enum SampleMode : int32_t {
-  kRowDone = 0,   // nothing is left to do
   kRowWhole = 1,  // every token is kept
   kRowFew = 2,    // all that may be kept are few: ranks lo .. hi
   kRowList = 3,   // the last kept token's eighth of an octave is ranks lo .. hi
@@ -75,7 +74,6 @@ struct SampleArgs {
   uint64_t* h_sum;    // [rows][chunks][kSampleBins]
   uint32_t* h_cnt;
   SampleRow* row;     // [rows]
-  SamplePlan* plan;   // [rows]
   uint64_t* list;     // [rows][kSampleList][2] ranks and weights
   int32_t parts;      // workgroups that list a row's tokens
   uint64_t* r_sum;    // [batch][chunks][2]: sums of what is left of the distribution, and of it whole

@@ -35,7 +35,7 @@ SampleWs sample_ws(int64_t batch, int64_t rows, int64_t vocab, bool bf16) {
   };
   const size_t n = (size_t)rows * w.chunks;
   w.row = take((size_t)rows * sizeof(SampleRow));
-  w.list = take((size_t)rows * kSampleList * 2 * sizeof(uint64_t));
+  w.list = take((size_t)rows * kSampleList * sizeof(uint64_t));
   w.c_top = take(n * sizeof(float));
   w.c_best = take(n * sizeof(uint64_t));
   w.c_sum = take(n * sizeof(uint64_t));

@@ -216,27 +216,32 @@ struct RowReader {
 __device__ __forceinline__ uint64_t shfl_xor_u64(uint64_t x, int d) {
   return (uint64_t)__shfl_xor((unsigned long long)x, d);
 }
+// One step of a scan over the wave in registers: x with the value that a DPP control moves here (`old` where none comes).
+template <int ctrl, int rows, class Op>
+__device__ __forceinline__ uint64_t dpp_step(uint64_t x, uint64_t old, Op op) {
+  const uint32_t lo = __builtin_amdgcn_update_dpp((int)(uint32_t)old, (int)(uint32_t)x, ctrl, rows, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp((int)(old >> 32), (int)(x >> 32), ctrl, rows, 0xf, false);
+  return op(x, ((uint64_t)hi << 32) | lo);
+}
+template <class Op>
+__device__ __forceinline__ uint64_t wave_scan(uint64_t x, uint64_t old, Op op) {  // inclusive
+  x = dpp_step<0x111, 0xf>(x, old, op);
+  x = dpp_step<0x112, 0xf>(x, old, op);
+  x = dpp_step<0x114, 0xf>(x, old, op);
+  x = dpp_step<0x118, 0xf>(x, old, op);
+  x = dpp_step<0x142, 0xa>(x, old, op);  // the rows' last lanes to the rows behind
+  return dpp_step<0x143, 0xc>(x, old, op);
+}
+__device__ __forceinline__ uint64_t last_lane(uint64_t x) {
+  return ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), kWave - 1) << 32) |
+         (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, kWave - 1);
+}
+__device__ __forceinline__ uint64_t wave_scan(uint64_t x) {
+  return wave_scan(x, 0, [](uint64_t p, uint64_t q) { return p + q; });
+}
+__device__ __forceinline__ uint64_t wave_sum(uint64_t x) { return last_lane(wave_scan(x)); }
 __device__ __forceinline__ uint64_t wave_min(uint64_t x) {
-#pragma unroll
-  for (int d = 1; d < kWave; d *= 2) {
-    const uint64_t y = shfl_xor_u64(x, d);
-    x = y < x ? y : x;
-  }
-  return x;
-}
-__device__ __forceinline__ uint64_t wave_sum(uint64_t x) {
-#pragma unroll
-  for (int d = 1; d < kWave; d *= 2) x += shfl_xor_u64(x, d);
-  return x;
-}
-__device__ __forceinline__ uint64_t wave_scan(uint64_t x) {  // inclusive
-  const int lane = threadIdx.x & (kWave - 1);
-#pragma unroll
-  for (int d = 1; d < kWave; d *= 2) {
-    const uint64_t y = (uint64_t)__shfl_up((unsigned long long)x, d);
-    if (lane >= d) x += y;
-  }
-  return x;
+  return last_lane(wave_scan(x, ~0ull, [](uint64_t p, uint64_t q) { return q < p ? q : p; }));
 }
 
 // Sum over a workgroup of `waves` waves, for every thread.
@@ -276,6 +281,29 @@ __device__ __forceinline__ double rescaled(const Exp2& exp2, float c_top, float 
 }
 __device__ __forceinline__ uint64_t scaled(uint64_t sum, double factor) {
   return factor == 1.0 ? sum : (uint64_t)((double)sum * factor);
+}
+
+// Both at once: the sums before this thread, and in all.
+struct Two {
+  uint64_t x, y;
+};
+template <int waves>
+__device__ __forceinline__ Two block_before(Two v, Two* sm, Two& all) {
+  const Two incl{wave_scan(v.x), wave_scan(v.y)};
+  __syncthreads();
+  if ((threadIdx.x & (kWave - 1)) == kWave - 1) sm[threadIdx.x / kWave] = incl;
+  __syncthreads();
+  Two base{0, 0};
+  all = base;
+#pragma unroll
+  for (int w = 0; w < waves; ++w) {
+    const Two o = sm[w];
+    base.x += w < (int)threadIdx.x / kWave ? o.x : 0;
+    base.y += w < (int)threadIdx.x / kWave ? o.y : 0;
+    all.x += o.x;
+    all.y += o.y;
+  }
+  return {base.x + incl.x - v.x, base.y + incl.y - v.y};
 }
 
 template <bool kBf16>
@@ -402,16 +430,27 @@ template <bool kBf16, class Value>
 __device__ int draw_in_chunk(const SampleArgs& a, const RowReader<kBf16>& row, int chunk, uint64_t target, Value value,
                              uint64_t* sm, int* sm_token) {
   constexpr int n = RowReader<kBf16>::n;
-  const int i0 = row.first(chunk * a.granules + (int)threadIdx.x);
-  auto at = [&](int i) -> uint64_t {
-    if (i < 0 || i >= a.vocab) return 0;
-    const float x = row.at(i);
-    return x == -INFINITY ? 0 : value(x, i);
+  const int g = chunk * a.granules + (int)threadIdx.x, i0 = row.first(g);
+  const bool is = (int)threadIdx.x < a.granules, inside = is && row.inside(g);
+  u32x4 bits = {0u, 0u, 0u, 0u};
+  if (inside) bits = row.bits(g);
+  auto at = [&](int e) -> uint64_t {
+    const int i = i0 + e;
+    float x;
+    if (inside) {
+      const int q = e * 4 / n;
+      const uint32_t y = q < 2 ? (q == 0 ? bits[0] : bits[1]) : (q == 2 ? bits[2] : bits[3]);
+      x = __uint_as_float(!kBf16 ? y : e & 1 ? y & 0xffff0000u : y << 16);
+    } else {
+      if (i < 0 || i >= a.vocab) return 0;
+      x = row.at(i);
+    }
+    return x == -INFINITY || x != x ? 0 : value(x, i);
   };
   uint64_t own = 0;
-  if ((int)threadIdx.x < a.granules)
+  if (is)
 #pragma unroll 1
-    for (int e = 0; e < n; ++e) own += at(i0 + e);
+    for (int e = 0; e < n; ++e) own += at(e);
   if (threadIdx.x == 0) *sm_token = -1;
   uint64_t all;
   uint64_t run = block_before<kRowWaves>(own, sm, all);
@@ -419,7 +458,7 @@ __device__ int draw_in_chunk(const SampleArgs& a, const RowReader<kBf16>& row, i
   if (run <= target && target < run + own)  // one thread's tokens
 #pragma unroll 1
     for (int e = 0; e < n; ++e) {
-      const uint64_t v = at(i0 + e);
+      const uint64_t v = at(e);
       if (run <= target && target < run + v) *sm_token = i0 + e;
       run += v;
     }
@@ -457,7 +496,9 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
   __shared__ unsigned long long sm_chunk_sum[kSampleMaxChunks];
   __shared__ double sm_factor[kSampleMaxChunks];
   __shared__ int sm_off[kSampleMaxChunks];
+  __shared__ unsigned long long sm_least[1024], sm_most[1024];  // ranks in them
   __shared__ uint64_t sm_red[kRowWaves], sm_u64[4];
+  __shared__ Two sm_two[kRowWaves];
   __shared__ int sm_int[2];
   const int r = blockIdx.y, tid = threadIdx.x;
   const int b = r / a.rows_per_seq, t = r - b * a.rows_per_seq;
@@ -523,17 +564,17 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
     }
     __syncthreads();
     const uint64_t my_cnt = tid < kSampleBins ? sm_cnt[tid] : 0, my_sum = tid < kSampleBins ? sm_sum[tid] : 0;
-    uint64_t all_cnt;
-    const uint64_t cnt_before = block_before<kRowWaves>(my_cnt, sm_red, all_cnt);
-    const uint64_t sum_before = block_before<kRowWaves>(my_sum, sm_red, all_sum);
-    // the eighth of an octave in which the kept set ends, by count or sum, and by min_p
-    const bool by_count = s.k > 0 && (uint64_t)s.k < all_cnt;
-    const bool count_scale = by_count || s.counts_do();
-    double target = by_count ? (double)s.k : s.counts_do() ? (double)all_cnt : s.p * (double)all_sum;
     if (tid == 0) sm_int[0] = kSampleBins - 1;
-    __syncthreads();
-    if (my_cnt && (count_scale ? (double)(cnt_before + my_cnt) : (double)(sum_before + my_sum)) >= target)
-      atomicMin(&sm_int[0], tid);
+    Two all;
+    const Two before = block_before<kRowWaves>(Two{my_cnt, my_sum}, sm_two, all);
+    all_sum = all.y;
+    // the eighth of an octave in which the kept set ends, by count or sum, and by min_p
+    const bool by_count = s.k > 0 && (uint64_t)s.k < all.x;
+    const bool count_scale = by_count || s.counts_do();
+    double target = by_count ? (double)s.k : s.counts_do() ? (double)all.x : s.p * (double)all_sum;
+    const double from = (double)(count_scale ? before.x : before.y);
+    const double upto = (double)(count_scale ? before.x + my_cnt : before.y + my_sum);
+    if (my_cnt && upto >= target && (from < target || tid == 0)) sm_int[0] = tid;  // one thread, or none
     __syncthreads();
     int bin = sm_int[0];
     if (s.m > 0.0) {
@@ -547,8 +588,8 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
       }
     }
     if (tid == bin) {  // (one that only min_p names may hold no token)
-      sm_u64[0] = cnt_before;
-      sm_u64[1] = sum_before;
+      sm_u64[0] = before.x;
+      sm_u64[1] = before.y;
       sm_u64[2] = my_cnt;
     }
     __syncthreads();
@@ -567,14 +608,16 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
   }
   const bool lists = plan.mode == kRowFew || plan.mode == kRowList;
   if (!lists && blockIdx.x > 0) return;
-  // calls f(rank, units) for every token of pieces [g0, g1) that has any and whose rank lies in [lo, hi]
+  // calls f(rank) for every token of pieces [g0, g1) whose rank lies in [lo, hi]
   auto each = [&](int g0, int g1, uint64_t lo, uint64_t hi, auto f) {
     const float x_hi = ceiling_of(lo), x_lo = bottom_of(hi);
 #pragma unroll 4
     for (int g = g0 + tid; g < g1; g += kRowThreads) {
+      u32x4 v = {0u, 0u, 0u, 0u};
       uint32_t hits = 0;
-      if (row.inside(g)) {
-        const u32x4 v = row.bits(g);
+      const bool inside = row.inside(g);
+      if (inside) {
+        v = row.bits(g);
 #pragma unroll
         for (int e = 0; e < n; ++e) {
           const float x = row.of_bits(v, e);
@@ -585,27 +628,31 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
         for (int e = 0; e < n; ++e) hits |= i0 + e >= 0 && i0 + e < a.vocab ? 1u << e : 0u;
       }
       while (hits) {
-        const int i = row.first(g) + __builtin_ctz(hits);
+        const int e = __builtin_ctz(hits), i = row.first(g) + e;
         hits &= hits - 1;
-        const float x = row.at(i);
+        float x;
+        if (inside) {
+          const int q = e * 4 / n;
+          const uint32_t y = q < 2 ? (q == 0 ? v[0] : v[1]) : (q == 2 ? v[2] : v[3]);
+          x = __uint_as_float(!kBf16 ? y : e & 1 ? y & 0xffff0000u : y << 16);
+        } else {
+          x = row.at(i);
+        }
         const uint64_t c = rank_of(x, i);
-        const uint64_t w = x != -INFINITY && c >= lo && c <= hi ? units_of(exp2, x, top, s.scale) : 0;
-        if (w) f(c, w);
+        if (x != -INFINITY && c >= lo && c <= hi) f(c);
       }
     }
   };
+  auto units_at = [&](uint64_t c) { return units_of(exp2, logit_of_rank(c), top, s.scale); };
   int m = 0;  // tokens in the list
   if (lists) {
     const int share = (pieces + a.parts - 1) / a.parts;
-    uint64_t* list = a.list + (int64_t)r * kList * 2;
+    uint64_t* list = a.list + (int64_t)r * kList;
     if (tid == 0) sm_cnt[0] = 0;
     __syncthreads();
-    each(blockIdx.x * share, min(pieces, (int)(blockIdx.x + 1) * share), plan.lo, plan.hi, [&](uint64_t c, uint64_t w) {
+    each(blockIdx.x * share, min(pieces, (int)(blockIdx.x + 1) * share), plan.lo, plan.hi, [&](uint64_t c) {
       const uint32_t at = atomicAdd(&sm_cnt[0], 1u);
-      if (at < kList) {
-        sm_rank[at] = c;
-        sm_w[at] = w;
-      }
+      if (at < kList) sm_rank[at] = c;
     });
     __syncthreads();
     m = min((int)sm_cnt[0], kList);
@@ -613,21 +660,15 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
       if (tid == 0) sm_cnt[1] = m ? __hip_atomic_fetch_add(&a.listed[r], (uint32_t)m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
       __syncthreads();
       const int base = (int)sm_cnt[1];
-      for (int j = tid; j < m && base + j < kList; j += kRowThreads) {
-        put(list + 2 * (base + j), sm_rank[j]);
-        put(list + 2 * (base + j) + 1, sm_w[j]);
-      }
-    }
-    if (!arrive_last(&a.arrived[r], a.parts, &sm_int[0])) return;
-    if (a.parts > 1) {
+      for (int j = tid; j < m && base + j < kList; j += kRowThreads) put(list + base + j, sm_rank[j]);
+      if (!arrive_last(&a.arrived[r], a.parts, &sm_int[0])) return;
       m = min((int)get(&a.listed[r]), kList);
-      for (int j = tid; j < m; j += kRowThreads) {
-        sm_rank[j] = get(list + 2 * j);
-        sm_w[j] = get(list + 2 * j + 1);
-      }
+      for (int j = tid; j < m; j += kRowThreads) sm_rank[j] = get(list + j);
       __syncthreads();
       if (tid == 0) put(&a.listed[r], 0u);
     }
+    for (int j = tid; j < m; j += kRowThreads) sm_w[j] = units_at(sm_rank[j]);
+    __syncthreads();
   }
   if (plan.mode == kRowFew && m <= kPairs) {
     // ---- few: each compared with each
@@ -682,7 +723,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
       for (int j = tid; j < m; j += kRowThreads)
         if (sm_rank[j] >= lo && sm_rank[j] <= hi) f(sm_rank[j], sm_w[j]);
     } else {
-      each(0, pieces, lo, hi, f);
+      each(0, pieces, lo, hi, [&](uint64_t c) { f(c, units_at(c)); });
     }
   };
   // the first token of ranks lo .. hi at which the running count (or sum), from what is before them, reaches the
@@ -691,53 +732,36 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
   auto find_token = [&](uint64_t lo, uint64_t hi, uint64_t cnt_b, uint64_t sum_b, bool by_sum, double target,
                         uint64_t& sum) {
     for (;;) {
-      // the ranks that there are
-      __syncthreads();
-      if (tid == 0) {
-        sm_u64[0] = ~0ull;
-        sm_u64[1] = 0;
-      }
-      __syncthreads();
-      if (lists) {
-        uint64_t least = ~0ull, most = 0;
-        each_token(lo, hi, [&](uint64_t c, uint64_t) {
-          least = c < least ? c : least;
-          most = c > most ? c : most;
-        });
-        least = wave_min(least);
-        most = ~wave_min(~most);
-        if ((tid & (kWave - 1)) == 0 && most >= least) {
-          atomicMin(reinterpret_cast<unsigned long long*>(&sm_u64[0]), (unsigned long long)least);
-          atomicMax(reinterpret_cast<unsigned long long*>(&sm_u64[1]), (unsigned long long)most);
-        }
-        __syncthreads();
-        lo = sm_u64[0];
-        hi = sm_u64[1];
-      }
       const int bits = hi == lo ? 0 : 64 - __clzll((long long)(hi - lo));
       const int shift = bits > 10 ? bits - 10 : 0;
       __syncthreads();
       sm_sum[tid] = 0;
       sm_cnt[tid] = 0;
+      sm_least[tid] = ~0ull;
+      sm_most[tid] = 0;
       if (tid == 0) {
-        sm_int[0] = 1 << 20;
+        sm_int[0] = -1;
         sm_int[1] = 0;
       }
       __syncthreads();
       each_token(lo, hi, [&](uint64_t c, uint64_t w) {
+        if (!w) return;
         const int j = (int)((c - lo) >> shift);
         atomicAdd(&sm_cnt[j], 1u);
         atomicAdd(&sm_sum[j], (unsigned long long)w);
+        atomicMin(&sm_least[j], (unsigned long long)c);
+        atomicMax(&sm_most[j], (unsigned long long)c);
       });
       __syncthreads();
       const uint64_t oc = sm_cnt[tid], os = sm_sum[tid];
-      uint64_t x;
-      const uint64_t cb = cnt_b + block_before<kRowWaves>(oc, sm_red, x);
-      const uint64_t sb = sum_b + block_before<kRowWaves>(os, sm_red, x);
-      if (oc && (by_sum ? (double)(sb + os) : (double)(cb + oc)) >= target) atomicMin(&sm_int[0], tid);
-      if (oc) atomicMax(&sm_int[1], tid);
+      Two all;
+      const Two before = block_before<kRowWaves>(Two{oc, os}, sm_two, all);
+      const uint64_t cb = cnt_b + before.x, sb = sum_b + before.y;
+      const double from = (double)(by_sum ? sb : cb), upto = (double)(by_sum ? sb + os : cb + oc);
+      if (oc && upto >= target && (from < target || before.x == 0)) sm_int[0] = tid;  // one thread, or none:
+      if (oc && before.x + oc == all.x) sm_int[1] = tid;                              // then the last that has any
       __syncthreads();
-      const int j = min(sm_int[0], sm_int[1]);
+      const int j = sm_int[0] < 0 ? sm_int[1] : sm_int[0];
       if (tid == j) {
         sm_u64[0] = cb;
         sm_u64[1] = sb;
@@ -748,10 +772,9 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
       cnt_b = sm_u64[0];
       sum_b = sm_u64[1];
       sum = sm_u64[2];
-      lo += (uint64_t)j << shift;
-      if (shift == 0) return lo;
-      const uint64_t end = lo + ((1ull << shift) - 1);
-      hi = end < hi ? end : hi;
+      lo = sm_least[j];
+      hi = sm_most[j];
+      if (lo >= hi) return lo;
       if (in > kCompare) continue;
       // few: each compared with each, in the histogram's place
       __syncthreads();
@@ -762,17 +785,18 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
       }
       __syncthreads();
       each_token(lo, hi, [&](uint64_t c, uint64_t w) {
+        if (!w) return;
         const int at = atomicAdd(&sm_int[0], 1);
         sm_sum[at] = c;
         sm_sum[kCompare + at] = w;
       });
       __syncthreads();
-      const int all = sm_int[0];
-      if (tid < all) {
+      const int few = sm_int[0];
+      if (tid < few) {
         const uint64_t c = sm_sum[tid], w = sm_sum[kCompare + tid];
         uint64_t cb2 = cnt_b + 1, sb2 = sum_b + w;
         uint64_t worse = 0;
-        for (int i = 0; i < all; ++i) {
+        for (int i = 0; i < few; ++i) {
           const bool better = sm_sum[i] < c;
           cb2 += better;
           sb2 += better ? sm_sum[kCompare + i] : 0;
@@ -783,9 +807,9 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
       }
       __syncthreads();
       const uint64_t found = sm_u64[0];
-      if (tid < all && sm_sum[tid] == found) {
+      if (tid < few && sm_sum[tid] == found) {
         uint64_t sb2 = sum_b;
-        for (int i = 0; i < all; ++i) sb2 += sm_sum[i] <= found ? sm_sum[kCompare + i] : 0;
+        for (int i = 0; i < few; ++i) sb2 += sm_sum[i] <= found ? sm_sum[kCompare + i] : 0;
         sm_u64[1] = sb2;
       }
       __syncthreads();

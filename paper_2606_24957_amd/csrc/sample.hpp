@@ -74,7 +74,7 @@ struct SampleArgs {
   uint64_t* h_sum;    // [rows][chunks][kSampleBins]
   uint32_t* h_cnt;
   SampleRow* row;     // [rows]
-  uint64_t* list;     // [rows][kSampleList][2] ranks and weights
+  uint64_t* list;     // [rows][kSampleList] ranks
   int32_t parts;      // workgroups that list a row's tokens
   uint64_t* r_sum;    // [batch][chunks][2]: sums of what is left of the distribution, and of it whole
   uint32_t* arrived;  // [rows], zero between calls

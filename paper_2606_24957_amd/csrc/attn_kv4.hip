@@ -4,13 +4,13 @@
 // A workgroup of eight waves takes an equal share of the batch's tokens: the tokens of all (sequence, KV head) pairs
 // lie end to end on one axis, in granules of 128, which is cut into as many equal runs as there are workgroups.  A run
 // may end inside a pair, or span several; the parts of a pair that several workgroups hold are joined by a second
-// kernel.  A part is done in rounds, of 32 tokens to a wave (16 from two tiles of query rows on):
+// kernel.  A part is done in rounds of 16 tokens to a wave:
 //   loads  a wave's rows of the rounds ahead go from memory straight into LDS as they are, 136 bytes a token
 //   S      the wave decodes its tokens' K rows into MFMA operands (lane: token, block; the channels of one 32-channel
 //          step are those of four blocks, and the queries are laid out to match): S^T = K Q^T for its tokens, all rows
 //   P      probabilities against a running reference of each row, the same in all waves, as operands of the value
 //          product into LDS; and its tokens' V rows, decoded, into a tile that all waves share
-//   O      after a barrier each wave adds all the round's tokens to 16 of the 128 channels: O^T += V^T P^T
+//   O      after the round's barrier each wave adds all the round's tokens to 16 of the 128 channels: O^T += V^T P^T
 // so that a wave holds an eighth of the accumulator, and nothing is left to add up at the end but the row sums.
 #include "kv4.hpp"
 
@@ -122,28 +122,32 @@ __device__ __forceinline__ int run_length(const Attn4Args& a, int total) {
 
 template <int RT, bool kSparse, bool kPaged>
 __global__ __launch_bounds__(kThreads4) void attn_kv4_kernel(Attn4Args a) {
-  constexpr int kTpw = RT == 1 ? 32 : 16;        // tokens of a wave's round
+  constexpr int kTpw = 16;                       // tokens of a wave's round
   constexpr int NT = kTpw / 16;
   constexpr int kTok = kW4 * kTpw;               // of a round
   constexpr int kRaw = kTpw * 136;               // a wave's rows and scales of a round as they come from memory
   constexpr int kRawLoads = 2 * NT + 1;
-  constexpr int kSlots = RT == 1 || RT > 6 ? 2 : 3;        // rounds in flight
+  constexpr int kSlots = RT <= 4 ? 3 : 2;        // rounds in flight
+  // Two V tiles and two sets of probabilities, so that a round's are written while others still read those of the round
+  // before: one barrier a round (where LDS holds them).
+  constexpr int kSets = RT <= 6 ? 2 : 1;
   constexpr int kExtra = (kSparse ? 1 : 0) + (kPaged ? 1 : 0);  // loads of positions and pages in a round
   constexpr bool kQReg = RT <= 6;                // the queries in registers, else read from LDS in every round
   constexpr int kQPitch = kD4 + 8;
   constexpr int kQBytes = RT * 16 * kQPitch * 2;
   constexpr int kVBytes = kTok * kD4 * 2;
   // (objects of their own: the loads in flight into one then hold back no read of another)
-  __shared__ __attribute__((aligned(1024))) char sm_v[kVBytes > kQBytes || !kQReg ? kVBytes : kQBytes];
+  static_assert(kQBytes <= kSets * kVBytes || !kQReg, "the queries pass through the V tiles");
+  __shared__ __attribute__((aligned(1024))) char sm_v[kSets * kVBytes];
   __shared__ __attribute__((aligned(16))) char sm_q_own[kQReg ? 16 : kQBytes];
-  __shared__ __attribute__((aligned(16))) char sm_p[RT * kTok * 32];  // [row tile][32 tokens][lane] of 16 bytes
+  __shared__ __attribute__((aligned(16))) char sm_p[kSets * RT * kTok * 32];  // [row tile][32 tokens][lane] of 16 bytes
   __shared__ __attribute__((aligned(1024))) char sm_raw[kW4 * kSlots * kRaw];
   __shared__ __attribute__((aligned(16))) char sm_pos[kSparse ? kW4 * kRing4 * kTpw * 4 : 16];
   __shared__ __attribute__((aligned(16))) char sm_page[kPaged ? kW4 * kRing4 * kTpw * 4 : 16];
   __shared__ __attribute__((aligned(16))) int sm_over[2][kW4];
   __shared__ float sm_max[kW4][RT * 16];
   __shared__ int sm_scan[kW4];
-  __shared__ int sm_first[2];
+  __shared__ int sm_first[5];
 
   const int lane = threadIdx.x & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -155,8 +159,14 @@ __global__ __launch_bounds__(kThreads4) void attn_kv4_kernel(Attn4Args a) {
   // ---- the workgroup's run of granules: every thread sums those of a few pairs
   const int ppt = (a.pairs + kThreads4 - 1) / kThreads4;
   const int p0 = min(a.pairs, (int)threadIdx.x * ppt), p1 = min(a.pairs, p0 + ppt);
-  int own = 0;
-  for (int p = p0; p < p1; ++p) own += pair_of<kSparse>(a, p).granules();
+  int own = 0, own_T = 0, own_body = 0, own_N = 0;
+  for (int p = p0; p < p1; ++p) {
+    const Pair4 x = pair_of<kSparse>(a, p);
+    if constexpr (kSparse) own_N = a.dims.len(div22(p, a.num_kv_heads));
+    own += x.granules();
+    own_T = x.T;
+    own_body = x.body;
+  }
   const int incl = wave_sum_incl(own);
   if (lane == kWave - 1) sm_scan[wave] = incl;
   lds_barrier4();
@@ -176,12 +186,21 @@ __global__ __launch_bounds__(kThreads4) void attn_kv4_kernel(Attn4Args a) {
   if (unit >= ((xcd + 1) * active + 7) / 8) return;
   const int start = unit * per, end = min(total_g, start + per);
   for (int p = p0; p < p1; ++p) {
-    const int n = ppt == 1 ? own : pair_of<kSparse>(a, p).granules();
-    if (before <= start && start < before + n) {
+    if (ppt > 1) {
+      const Pair4 x = pair_of<kSparse>(a, p);
+      own = x.granules();
+      own_T = x.T;
+      own_body = x.body;
+      own_N = a.dims.len(div22(p, a.num_kv_heads));
+    }
+    if (before <= start && start < before + own) {
       sm_first[0] = p;
       sm_first[1] = before;
+      sm_first[2] = own_T;
+      sm_first[3] = own_body;
+      sm_first[4] = kSparse ? own_N : own_body;
     }
-    before += n;
+    before += own;
   }
   lds_barrier4();
   int pair = __builtin_amdgcn_readfirstlane(sm_first[0]);
@@ -190,8 +209,16 @@ __global__ __launch_bounds__(kThreads4) void attn_kv4_kernel(Attn4Args a) {
 
   for (int g0 = start; g0 < end; ++pair) {
     const int b = div22(pair, a.num_kv_heads), g = pair - b * a.num_kv_heads;
-    const Pair4 pr = pair_of<kSparse>(a, pair);
-    const int N = a.dims.len(b);
+    Pair4 pr;
+    int N;
+    if (g0 == start) {  // the first pair's sizes have been found
+      pr.T = __builtin_amdgcn_readfirstlane(sm_first[2]);
+      pr.body = __builtin_amdgcn_readfirstlane(sm_first[3]);
+      N = __builtin_amdgcn_readfirstlane(sm_first[4]);
+    } else {
+      pr = pair_of<kSparse>(a, pair);
+      N = a.dims.len(b);
+    }
     const int n_g = pr.granules();
     if (n_g == 0) continue;
     const int pair_end = pair_g + n_g;
@@ -308,6 +335,7 @@ __global__ __launch_bounds__(kThreads4) void attn_kv4_kernel(Attn4Args a) {
       for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) qreg[rt][ks] = read_q(rt, ks);
+    if constexpr (kQReg) lds_barrier4();  // (they were in the V tiles' place)
     int limit[RT];  // token v is visible to this lane's row iff v <= limit
     float m_ref[RT], l_sum[RT];  // the row's reference (the same in every wave), and the sum over this lane's tokens
     f32x4 acc[RT];  // channels 16 wave + 4 lg + e of row lr
@@ -321,117 +349,118 @@ __global__ __launch_bounds__(kThreads4) void attn_kv4_kernel(Attn4Args a) {
     }
     // Place of chunk c (8 channels) of token j of the V tile: the transpose loads of 16 tokens x 32 bytes, and the
     // stores of 16 tokens x 16 bytes, spread over all banks.
-    auto v_at = [&](int j, int c) { return sm_v + j * 256 + 16 * (c ^ (((j & 7) << 1) | ((j >> 3) & 1))); };
+    auto v_at = [&](int set, int j, int c) { return sm_v + set * kVBytes + j * 256 + 16 * (c ^ (((j & 7) << 1) | ((j >> 3) & 1))); };
     const uint32_t raw_lane = lds_addr(raw) + 16 * lane, raw_scale = lds_addr(raw) + kTpw * 128 + 4 * lr + lg;
     // this wave's probabilities in sm_p: operand bytes of its 32 tokens (or half of them)
-    char* const p_own = sm_p + (NT == 2 ? wave : wave / 2) * 1024 + lane * 16 + (NT == 2 ? 0 : 8 * (wave & 1));
+    char* const p_own = sm_p + wave / 2 * 1024 + lane * 16 + 8 * (wave & 1);
     constexpr int kPTile = kTok / 32 * 1024;  // bytes of a row tile
+    constexpr int kPSet = RT * kPTile;
 
     const int rounds = (t_end - t_begin + kTok - 1) / kTok;
     int slot_n = 0;
-    for (int n = 0; n < rounds; ++n) {
+    f32x4 sc[RT];    // scores of the round whose probabilities are in LDS: tokens 4 lg + e of row lr
+    u32x2 p_op[RT];  // its probabilities as operands, and their sums
+    float p_sum[RT];
+    auto probabilities = [&](int rt) {
+      float p[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) p[e] = fast_exp2(fmaf(sc[rt][e], a.scale_log2, -m_ref[rt]));
+      p_op[rt] = u32x2{pk_bf16(p[0], p[1]), pk_bf16(p[2], p[3])};
+      p_sum[rt] = (p[0] + p[1]) + (p[2] + p[3]);
+    };
+    auto own_max = [&](int rt) {
+      return fmaxf(fmaxf(sc[rt][0], sc[rt][1]), fmaxf(sc[rt][2], sc[rt][3])) * a.scale_log2;
+    };
+    auto write_p = [&](int set) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) *reinterpret_cast<u32x2*>(p_own + set * kPSet + rt * kPTile) = p_op[rt];
+    };
+    // O^T of 16 channels: token 32 k + 4 lg + e, and 32 k + 16 + 4 lg + e
+    const int j0 = 4 * lg + (lr >> 2), c_own = 2 * wave + ((lr >> 1) & 1);
+    constexpr int kSteps = kTok / 32;
+    bf16x8 vt[kSteps];
+    auto read_v = [&](int set) {
+#pragma unroll
+      for (int k = 0; k < kSteps; ++k) {
+        const u32x2 lo = read_tr16(v_at(set, 32 * k + j0, c_own) + 8 * (lr & 1));
+        const u32x2 hi = read_tr16(v_at(set, 32 * k + j0 + 16, c_own) + 8 * (lr & 1));
+        vt[k] = as_bf16x8(u32x4{lo[0], lo[1], hi[0], hi[1]});
+      }
+    };
+    auto add_round = [&](int set) {
+#pragma unroll
+      for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+          acc[rt] = mfma16x16x32(vt[k],
+                                 as_bf16x8(*reinterpret_cast<const u32x4*>(sm_p + set * kPSet + rt * kPTile + k * 1024 +
+                                                                           lane * 16)),
+                                 acc[rt]);
+    };
+    // One turn: the values of round n - 1 are added up (its probabilities and V tile are complete: `add`), while round
+    // n's rows are decoded, scored and written for the others (`next`).  Both are independent work between two
+    // barriers, for the waves' latencies to hide behind each other.
+    auto turn = [&](int n, bool add, bool next) {
+      const int set = kSets == 2 ? n & 1 : 0, before = kSets == 2 ? set ^ 1 : 0;
       if constexpr (!kQReg) asm volatile("" ::: "memory");  // the queries stay in LDS
-      // this round's rows, and the positions and pages that the loads below read
-      wait_loads<(kSlots - 1) * kRawLoads + kExtra>();
-      u32x4 kd[NT], vd[NT];
-      uint32_t kse[NT], vse[NT];
-      if constexpr (NT == 2)
-        asm volatile(
-            "ds_read_b128 %0, %8\n\tds_read_b128 %1, %8 offset:1024\n\tds_read_b128 %2, %8 offset:2048\n\t"
-            "ds_read_b128 %3, %8 offset:3072\n\tds_read_u8 %4, %9\n\tds_read_u8 %5, %9 offset:64\n\t"
-            "ds_read_u8 %6, %9 offset:128\n\tds_read_u8 %7, %9 offset:192\n\ts_waitcnt lgkmcnt(0)"
-            : "=&v"(kd[0]), "=&v"(kd[NT - 1]), "=&v"(vd[0]), "=&v"(vd[NT - 1]), "=&v"(kse[0]), "=&v"(kse[NT - 1]),
-              "=&v"(vse[0]), "=&v"(vse[NT - 1])
-            : "v"(raw_lane + slot_n * kRaw), "v"(raw_scale + slot_n * kRaw)
-            : "memory");
-      else
+      if (add) read_v(before);
+      if constexpr (kSets == 1) {  // one set: read it whole before it is written again
+        if (add) add_round(before);
+        lds_barrier4();
+      }
+      bf16x8 kop[4];
+      if (next) {
+        // this round's rows, and the positions and pages that the loads below read
+        wait_loads<(kSlots - 1) * kRawLoads + kExtra>();
+        u32x4 kd, vd;
+        uint32_t kse, vse;
         asm volatile(
             "ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:1024\n\tds_read_u8 %2, %5\n\t"
             "ds_read_u8 %3, %5 offset:64\n\ts_waitcnt lgkmcnt(0)"
-            : "=&v"(kd[0]), "=&v"(vd[0]), "=&v"(kse[0]), "=&v"(vse[0])
+            : "=&v"(kd), "=&v"(vd), "=&v"(kse), "=&v"(vse)
             : "v"(raw_lane + slot_n * kRaw), "v"(raw_scale + slot_n * kRaw)
             : "memory");
-      load_pos(n + kSlots + 4);
-      load_page(n + kSlots + 2);
-      load_rows(n + kSlots, slot_n);
-      slot_n = slot_n + 1 == kSlots ? 0 : slot_n + 1;
-
-      // ---- scores: lane holds tokens 16 i + 4 lg + e of row lr
-      bf16x8 kop[NT][4];
 #pragma unroll
-      for (int i = 0; i < NT; ++i)
+        for (int w = 0; w < 4; ++w)
+          *reinterpret_cast<u32x4*>(v_at(set, wave * kTpw + lr, 4 * lg + w)) = kv4_decode8(vd[w], kv4_scale(vse));
+        load_pos(n + kSlots + 4);
+        load_page(n + kSlots + 2);
+        load_rows(n + kSlots, slot_n);
+        slot_n = slot_n + 1 == kSlots ? 0 : slot_n + 1;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) kop[i][w] = as_bf16x8(kv4_decode8(kd[i][w], kv4_scale(kse[i])));
-      f32x4 sc[RT][NT];
+        for (int w = 0; w < 4; ++w) kop[w] = as_bf16x8(kv4_decode8(kd[w], kv4_scale(kse)));
+      }
+      if constexpr (kSets == 2)
+        if (add) add_round(before);
+      if (!next) return;
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
+      for (int rt = 0; rt < RT; ++rt) {
+        f32x4 c = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < NT; ++i) {
-          f32x4 c = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int ks = 0; ks < 4; ++ks) {
-            if constexpr (kQReg) c = mfma16x16x32(kop[i][ks], qreg[rt][ks], c);
-            else c = mfma16x16x32(kop[i][ks], read_q(rt, ks), c);
-          }
-          sc[rt][i] = c;
+        for (int ks = 0; ks < 4; ++ks) {
+          if constexpr (kQReg) c = mfma16x16x32(kop[ks], qreg[rt][ks], c);
+          else c = mfma16x16x32(kop[ks], read_q(rt, ks), c);
         }
+        sc[rt] = c;
+      }
       const int v0 = t_begin + n * kTok + wave * kTpw;
       if (v0 + kTpw - 1 >= min(wstart, t_end))  // wave-uniform: masking only near the window and the end
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-          for (int i = 0; i < NT; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (v0 + 16 * i + 4 * lg + e > min(limit[rt], t_end - 1)) sc[rt][i][e] = -INFINITY;
-
-      // ---- probabilities
-      u32x2 p_op[RT][NT];
-      float p_sum[RT];
-      auto probabilities = [&](int rt) {
-        float s[NT];
-#pragma unroll
-        for (int i = 0; i < NT; ++i) {
-          float p[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) p[e] = fast_exp2(fmaf(sc[rt][i][e], a.scale_log2, -m_ref[rt]));
-          p_op[rt][i] = u32x2{pk_bf16(p[0], p[1]), pk_bf16(p[2], p[3])};
-          s[i] = (p[0] + p[1]) + (p[2] + p[3]);
-        }
-        p_sum[rt] = NT == 2 ? s[0] + s[NT - 1] : s[0];
-      };
-      auto own_max = [&](int rt) {
-        float m = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < NT; ++i)
-          m = fmaxf(m, fmaxf(fmaxf(sc[rt][i][0], sc[rt][i][1]), fmaxf(sc[rt][i][2], sc[rt][i][3])));
-        return m * a.scale_log2;
-      };
+          for (int e = 0; e < 4; ++e)
+            if (v0 + 4 * lg + e > min(limit[rt], t_end - 1)) sc[rt][e] = -INFINITY;
       bool over = false;
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         probabilities(rt);
         over |= own_max(rt) > m_ref[rt] + kRescale4;
       }
-      auto write_p = [&]() {
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          if constexpr (NT == 2)
-            *reinterpret_cast<u32x4*>(p_own + rt * kPTile) =
-                u32x4{p_op[rt][0][0], p_op[rt][0][1], p_op[rt][NT - 1][0], p_op[rt][NT - 1][1]};
-          else *reinterpret_cast<u32x2*>(p_own + rt * kPTile) = p_op[rt][0];
-        }
-      };
-      lds_barrier4();  // the waves are done with the round before
-#pragma unroll
-      for (int i = 0; i < NT; ++i)
-#pragma unroll
-        for (int w = 0; w < 4; ++w)
-          *reinterpret_cast<u32x4*>(v_at(wave * kTpw + 16 * i + lr, 4 * lg + w)) =
-              kv4_decode8(vd[i][w], kv4_scale(vse[i]));
-      write_p();
+      write_p(set);
       const int any_over = __any(over) ? 1 : 0;
       if (lane == 0) sm_over[n & 1][wave] = any_over;
+    };
+    auto settle = [&](int n) {  // round n's probabilities are complete, against references that all waves agree on
       lds_barrier4();
       const u32x4 o0 = *reinterpret_cast<const u32x4*>(&sm_over[n & 1][0]);
       const u32x4 o1 = *reinterpret_cast<const u32x4*>(&sm_over[n & 1][4]);
@@ -455,27 +484,19 @@ __global__ __launch_bounds__(kThreads4) void attn_kv4_kernel(Attn4Args a) {
           acc[rt] *= alpha;
           probabilities(rt);
         }
-        write_p();
+        write_p(kSets == 2 ? n & 1 : 0);
         lds_barrier4();
       }
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) l_sum[rt] += p_sum[rt];
-
-      // ---- O^T of 16 channels: token 32 k + 4 lg + e, and 32 k + 16 + 4 lg + e
-      const int left = t_end - (t_begin + n * kTok);
-      const int j0 = 4 * lg + (lr >> 2), c = 2 * wave + ((lr >> 1) & 1);
-#pragma unroll
-      for (int k = 0; k < kTok / 32; ++k) {
-        if (k > 0 && 32 * k >= left) break;
-        const u32x2 lo = read_tr16(v_at(32 * k + j0, c) + 8 * (lr & 1));
-        const u32x2 hi = read_tr16(v_at(32 * k + j0 + 16, c) + 8 * (lr & 1));
-        const bf16x8 vt = as_bf16x8(u32x4{lo[0], lo[1], hi[0], hi[1]});
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-          acc[rt] = mfma16x16x32(
-              vt, as_bf16x8(*reinterpret_cast<const u32x4*>(sm_p + rt * kPTile + k * 1024 + lane * 16)), acc[rt]);
-      }
+    };
+    turn(0, false, true);
+    settle(0);
+    for (int n = 1; n < rounds; ++n) {
+      turn(n, true, true);
+      settle(n);
     }
+    turn(rounds, true, false);
     wait_loads<0>();
 
     // ---- the rows' sums over all waves, and the outputs
@@ -510,13 +531,14 @@ __global__ __launch_bounds__(kThreads4) void attn_kv4_kernel(Attn4Args a) {
   }
 }
 
-// Joins the parts of a pair: a workgroup for a query row, eight parts at a time, four channels to a thread; the eight
-// sums are added in order.
-template <bool kSparse>
+// Joins the parts of a pair.  32 threads add up a query row's parts (four channels each), or every eighth of them where
+// a pair has many parts, of which a second step adds the eight sums; always in order.
+template <bool kSparse, bool kMany>
 __global__ __launch_bounds__(256) void attn_kv4_merge_kernel(Attn4Args a) {
-  __shared__ f32x4 sm_acc[8][32];
+  __shared__ f32x4 sm_acc[kMany ? 8 : 1][32];
   __shared__ float sm_l[8];
-  const int pair = blockIdx.x, r = blockIdx.y;
+  const int group = threadIdx.x / 32, c0 = (threadIdx.x % 32) * 4;
+  const int pair = blockIdx.x, r = kMany ? blockIdx.y : blockIdx.y * 8 + group;
   const int b = div22(pair, a.num_kv_heads), g = pair - b * a.num_kv_heads;
   const Pair4 pr = pair_of<kSparse>(a, pair);
   const int per = a.plan[0], first = a.plan[1 + pair];
@@ -524,7 +546,6 @@ __global__ __launch_bounds__(256) void attn_kv4_merge_kernel(Attn4Args a) {
   if (n_g == 0 || r >= pr.T * a.group_size) return;
   const int u0 = first / per, u1 = (first + n_g - 1) / per;
   if (u0 == u1) return;
-  const int part = threadIdx.x / 32, c0 = (threadIdx.x % 32) * 4;
   auto slot_of = [&](int u) { return ((int64_t)2 * u + (u == u0 && u0 * per < first ? 1 : 0)) * a.rows_max + r; };
   float M = kNoRef;
   for (int u = u0 + (threadIdx.x & 31); u <= u1; u += 32) M = fmaxf(M, a.part_ml[slot_of(u)].x);
@@ -532,21 +553,24 @@ __global__ __launch_bounds__(256) void attn_kv4_merge_kernel(Attn4Args a) {
   for (int d = 1; d < 32; d *= 2) M = fmaxf(M, __shfl_xor(M, d));
   f32x4 x = {0.f, 0.f, 0.f, 0.f};
   float L = 0.f;
-  for (int u = u0 + part; u <= u1; u += 8) {
+#pragma unroll 4
+  for (int u = u0 + (kMany ? group : 0); u <= u1; u += kMany ? 8 : 1) {
     const int64_t s = slot_of(u);
     const float2 ml = a.part_ml[s];
     const float w = fast_exp2(ml.x - M);
     L += w * ml.y;
     x += w * *reinterpret_cast<const f32x4*>(a.part + s * kD4 + c0);
   }
-  sm_acc[part][threadIdx.x % 32] = x;
-  if (c0 == 0) sm_l[part] = L;
-  __syncthreads();
-  if (threadIdx.x >= 32) return;
-  L = sm_l[0];
-  for (int i = 1; i < 8; ++i) {
-    x += sm_acc[i][threadIdx.x];
-    L += sm_l[i];
+  if constexpr (kMany) {
+    sm_acc[group][threadIdx.x % 32] = x;
+    if (c0 == 0) sm_l[group] = L;
+    __syncthreads();
+    if (threadIdx.x >= 32) return;
+    L = sm_l[0];
+    for (int i = 1; i < 8; ++i) {
+      x += sm_acc[i][threadIdx.x];
+      L += sm_l[i];
+    }
   }
   x *= 1.f / L;
   const int t = div22(r, a.group_size), hh = r - t * a.group_size;
@@ -565,8 +589,12 @@ hipError_t launch_rt(const Attn4Args& a, int rt, hipStream_t stream) {
 #undef CASE
     default: return hipErrorInvalidValue;
   }
-  hipLaunchKernelGGL((attn_kv4_merge_kernel<kSparse>), dim3((unsigned)a.pairs, (unsigned)a.rows_max), dim3(256), 0,
-                     stream, a);
+  if (a.units > 8 * a.pairs)  // many parts to a pair
+    hipLaunchKernelGGL((attn_kv4_merge_kernel<kSparse, true>), dim3((unsigned)a.pairs, (unsigned)a.rows_max), dim3(256), 0,
+                       stream, a);
+  else
+    hipLaunchKernelGGL((attn_kv4_merge_kernel<kSparse, false>), dim3((unsigned)a.pairs, (unsigned)(a.rows_max + 7) / 8),
+                       dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 

@@ -5,7 +5,6 @@
 namespace dustin {
 
 constexpr int kEvictThreads = 256;    // out of place
-constexpr int kEvictPer = 4;          // 16-byte chunks of a thread, loaded before the first is stored
 constexpr int kEvictRunThreads = 1024;  // in place, and the weights
 constexpr int kEvictRunPer = 8;
 
@@ -47,8 +46,11 @@ __device__ __forceinline__ void evict_weights(const EvictArgs& a, int row) {
   }
 }
 
-// Out of place: one thread moves kEvictPer 16-byte chunks; consecutive threads take a row's chunks, its K and its V,
-// then the next KV head (K and V rows that lie side by side are then read and written as one).
+// Out of place: one thread moves a 16-byte chunk; consecutive threads take a row's chunks, its K and its V, then the
+// next KV head (K and V rows that lie side by side are then read and written as one).  Bound by memory and, for one
+// sequence, by the chain count, position, (page,) row: 8192 of 32768 positions, 8 KV heads, bf16, 22.8 us (2.9 TB/s);
+// with 2, 4 and 8 chunks to a thread, loaded before the first is stored, 24.8, 27.1 and 36.2: the more workgroups, the
+// more of one's loads run beside another's stores.  Stores past the caches: 27.3.
 template <int CPR>  // 16-byte chunks of a row
 __global__ __launch_bounds__(kEvictThreads) void evict_kernel(EvictArgs a, uint32_t parts, uint32_t extra) {
   if (blockIdx.x < extra) {
@@ -59,42 +61,23 @@ __global__ __launch_bounds__(kEvictThreads) void evict_kernel(EvictArgs a, uint3
   const int b = (int)(blk / parts);
   const uint32_t part = blk - (uint32_t)b * parts;
   const uint32_t H = (uint32_t)a.num_kv_heads;
-  u32x4 x[kEvictPer];
-  uint32_t sc[kEvictPer];
-  int64_t to[kEvictPer], sto[kEvictPer];
-  bool ok[kEvictPer], is_v[kEvictPer];
-#pragma unroll
-  for (int j = 0; j < kEvictPer; ++j) {
-    const uint32_t e = (part * kEvictPer + j) * kEvictThreads + threadIdx.x;
-    const uint32_t chunk = e % CPR, r = e / (2 * CPR);
-    is_v[j] = (e / CPR) & 1;
-    const uint32_t i = r / H, h = r - i * H;
-    const int go = a.groups == 1 ? 0 : (int)h;
-    ok[j] = i < (uint32_t)clampi(a.count[b * a.groups + go], 0, a.k_max);
-    if (!ok[j]) continue;
-    const EvictCache &s = a.src[is_v[j]], &d = a.dst[is_v[j]];
-    const int pos = clampi(a.idx[b * a.idx_sb + go * a.idx_sg + i], 0, s.cap_m1);
-    int64_t soff, doff;
-    const int64_t from = evict_row(s, b, pos, soff);
-    to[j] = evict_row(d, b, (int)i, doff) + h * d.stride_h + 16 * chunk;
-    sto[j] = doff + h * d.sstride_h;
-    x[j] = *reinterpret_cast<const u32x4*>(s.data + from + h * s.stride_h + 16 * chunk);
-    if (s.scales && chunk == 0) {
-      const uint8_t* p = s.scales + soff + h * s.sstride_h;
-      sc[j] = a.scale_bytes == 4 ? *reinterpret_cast<const uint32_t*>(p) : *reinterpret_cast<const uint16_t*>(p);
-    }
-  }
-#pragma unroll
-  for (int j = 0; j < kEvictPer; ++j) {
-    if (!ok[j]) continue;
-    const EvictCache& d = a.dst[is_v[j]];
-    const uint32_t chunk = ((part * kEvictPer + j) * kEvictThreads + threadIdx.x) % CPR;
-    *reinterpret_cast<u32x4*>(const_cast<uint8_t*>(d.data) + to[j]) = x[j];
-    if (d.scales && chunk == 0) {
-      uint8_t* p = const_cast<uint8_t*>(d.scales) + sto[j];
-      if (a.scale_bytes == 4) *reinterpret_cast<uint32_t*>(p) = sc[j];
-      else *reinterpret_cast<uint16_t*>(p) = (uint16_t)sc[j];
-    }
+  const uint32_t e = part * kEvictThreads + threadIdx.x;
+  const uint32_t chunk = e % CPR, r = e / (2 * CPR);
+  const int is_v = (e / CPR) & 1;
+  const uint32_t i = r / H, h = r - i * H;
+  const int go = a.groups == 1 ? 0 : (int)h;
+  if (i >= (uint32_t)clampi(a.count[b * a.groups + go], 0, a.k_max)) return;
+  const EvictCache &s = a.src[is_v], &d = a.dst[is_v];
+  const int pos = clampi(a.idx[b * a.idx_sb + go * a.idx_sg + i], 0, s.cap_m1);
+  int64_t soff, doff;
+  const int64_t from = evict_row(s, b, pos, soff), to = evict_row(d, b, (int)i, doff);
+  const u32x4 x = *reinterpret_cast<const u32x4*>(s.data + from + h * s.stride_h + 16 * chunk);
+  *reinterpret_cast<u32x4*>(const_cast<uint8_t*>(d.data) + to + h * d.stride_h + 16 * chunk) = x;
+  if (s.scales && chunk == 0) {
+    const uint8_t* p = s.scales + soff + h * s.sstride_h;
+    uint8_t* q = const_cast<uint8_t*>(d.scales) + doff + h * d.sstride_h;
+    if (a.scale_bytes == 4) *reinterpret_cast<uint32_t*>(q) = *reinterpret_cast<const uint32_t*>(p);
+    else *reinterpret_cast<uint16_t*>(q) = *reinterpret_cast<const uint16_t*>(p);
   }
 }
 
@@ -175,7 +158,7 @@ hipError_t launch_evict(const EvictArgs& a, hipStream_t stream) {
     return hipGetLastError();
   }
   const int64_t chunks = (int64_t)a.k_max * a.num_kv_heads * 2 * cpr;
-  const int64_t parts = (chunks + kEvictThreads * kEvictPer - 1) / (kEvictThreads * kEvictPer);
+  const int64_t parts = (chunks + kEvictThreads - 1) / kEvictThreads;
   grid = extra + parts * a.batch;
   if (grid > INT32_MAX / kEvictThreads || chunks > INT32_MAX) return hipErrorInvalidValue;
   if (grid == 0) return hipSuccess;

@@ -14,6 +14,10 @@
  * against (Efficiency baselines; Appendix G).  Around the attention, dustin_kv_append
  * writes the verification window's K and V into the caches (per layer, before step 4)
  * and dustin_kv_commit keeps the accepted window tokens after verification.
+ * The target's caches may be held in 4 bits: dustin_kv4_append, dustin_kv4_read and the _kv4 attention take the place of
+ * their bf16 counterparts (the scoring layer keeps its keys in bf16 beside them).  dustin_sample draws tokens from logits
+ * and dustin_verify_sample accepts or rejects a window's drafts (what dustin_kv_commit then keeps); dustin_kv_evict cuts
+ * caches to the positions with the most accumulated attention.
  * dustin_page_meta and dustin_page_score are the page estimator the paper compares its
  * scoring heads with (page-level key minima and maxima; Quest-16 in the estimation
  * overhead analysis): they produce an importance array that step 3 takes in place of,
@@ -567,7 +571,8 @@ dustin_status dustin_dense_verify_attn_kv4(const void* q, int64_t q_sb, int64_t 
  *   k, v, k_out, v_out  caches of 64 or 128 channels.  k_out and v_out are other caches (other pages), or the same:
  *       equal data, strides and page tables mark the call as in place.  Caches that overlap in another way are not
  *       supported, nor is one of K and V in place alone (DUSTIN_ERR_INVALID_ARG).  k_out and v_out address at least
- *       k_max positions.
+ *       k_max positions.  v and v_out may be NULL (a cache of keys alone, as the scores read); one cache must not be
+ *       given as both k and v.
  *   idx, count  int32 [B, groups, >= k_max] (strides idx_sb, idx_sg) and [B * groups]; ascending positions (in place,
  *       others give rows of unspecified content); groups 1 or the KV head count
  *   w, w_out    fp32 [B, groups, >= w_len], [B, groups, >= k_max] (strides in elements) or both NULL; w_out may be w

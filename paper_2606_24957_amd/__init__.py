@@ -10,6 +10,10 @@ Step of one speculative verification (paper: method section 4, Eqs. 5 and 6):
     s_d = score(q_draft[l], k_draft[l], seq_lens, draft_heads, init=s_d)     # S_Draft, per layer
     idx, cnt = topk(s_d, s_t, seq_lens, k_max, m_scalar=m)                   # I_verify
     o[l] = sparse_verify_attn(q[l], k[l], v[l], idx, cnt, seq_lens)          # every layer
+    keep, token = verify_tokens(logits, draft, u_accept, u)                  # accepted drafts, next token
+    kv_commit(seq_lens, keep, nq_max=T)
+A layer's caches may be held in 4 bits (KV4: kv4_append, sparse_verify_attn_kv4), and all of them cut to the positions
+with the most accumulated attention (kv_evict).
 """
 from __future__ import annotations
 
@@ -1048,11 +1052,16 @@ def plan_kv_evict(k, v, idx: torch.Tensor, count: torch.Tensor, *, k_out=None, v
                   weights: Optional[torch.Tensor] = None, weights_out: Optional[torch.Tensor] = None,
                   new_lens: Optional[torch.Tensor] = None, stream=None) -> Call:
     """Prepared dustin_kv_evict (bf16 caches) or dustin_kv4_evict (KV4): a layer's rows idx[b, g, :count] to the front
-    of k_out / v_out (with out_page_table), or of the caches themselves where no outputs are given.  weights fp32
+    of k_out / v_out (with out_page_table), or of the caches themselves where no outputs are given.  v None: k alone
+    (a cache of keys that the scores read).  weights fp32
     [B, G, N] go the same way into weights_out (None: in place), new_lens int32 [B] becomes the counts."""
     four = isinstance(k, KV4)
-    if (k_out is None) != (v_out is None) or any(isinstance(x, KV4) != four for x in (v, k_out, v_out) if x is not None):
-        raise ValueError("k, v, k_out and v_out are bf16 caches or KV4 caches, both outputs or neither given")
+    if any(isinstance(x, KV4) != four for x in (v, k_out, v_out) if x is not None):
+        raise ValueError("k, v, k_out and v_out are bf16 caches or KV4 caches")
+    if (v is not None and (k_out is None) != (v_out is None)) or (v is None and v_out is not None):
+        raise ValueError("outputs for each of the caches, or for none")
+    if v is not None and (k.data if four else k).data_ptr() == (v.data if four else v).data_ptr():
+        raise ValueError("k and v are one cache: give it as k alone")
     if k_out is None:
         if out_page_table is not None:
             raise ValueError("in place, the pages stay: out_page_table goes with outputs")
@@ -1063,11 +1072,11 @@ def plan_kv_evict(k, v, idx: torch.Tensor, count: torch.Tensor, *, k_out=None, v
     tables = [None if t is None else t.contiguous() for t in (page_table, out_page_table)]
     if page_table is out_page_table:
         tables[1] = tables[0]
-    if four:
-        views = [x for pair, t in zip(((k, v), (k_out, v_out)), tables) for x in _kv4_pair(*pair, t)]
-    else:
-        _on_gpu(k, v, k_out, v_out, page_table, out_page_table)
-        views = [kv_view(x, t) for pair, t in zip(((k, v), (k_out, v_out)), tables) for x in pair]
+    view, views = (kv4_view if four else kv_view), []
+    for pair, t in zip(((k, v), (k_out, v_out)), tables):
+        for x in pair:
+            _on_gpu(*(x if four and x is not None else (x,)), t)
+            views.append(None if x is None else view(x, t))
     for x, t in zip((k, k_out), tables):
         n = t.shape[0] if t is not None else (x.data if four else x).shape[0]
         if n < B:
@@ -1087,7 +1096,7 @@ def plan_kv_evict(k, v, idx: torch.Tensor, count: torch.Tensor, *, k_out=None, v
     if new_lens is not None and (new_lens.dtype != torch.int32 or new_lens.numel() < B or not new_lens.is_contiguous()):
         raise ValueError("new_lens must be a contiguous int32 [B] tensor")
     what = "dustin_kv4_evict" if four else "dustin_kv_evict"
-    args = (*(ctypes.byref(x) for x in views), B, _ptr(idx), idx.stride(0), idx.stride(1), _ptr(count), G, k_max,
+    args = (*(None if x is None else ctypes.byref(x) for x in views), B, _ptr(idx), idx.stride(0), idx.stride(1), _ptr(count), G, k_max,
             _ptr(weights), ws[0], ws[1], ws[2], _ptr(weights_out), ws[3], ws[4], _ptr(new_lens), _stream(stream))
     keep = (k, v, k_out, v_out, idx, count, tables, views, weights, weights_out, new_lens)
     return Call(getattr(lib(), what), args, what, keep, (k_out, v_out))

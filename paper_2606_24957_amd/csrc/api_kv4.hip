@@ -230,8 +230,8 @@ dustin_status evict(const Kv* k, const Kv* v, const Kv* k_out, const Kv* v_out, 
                     int64_t idx_sb, int64_t idx_sg, const int32_t* count, int32_t groups, int32_t k_max, const float* w,
                     int64_t w_sb, int64_t w_sg, int32_t w_len, float* w_out, int64_t wo_sb, int64_t wo_sg,
                     int32_t* new_lens, int row_bytes_per_dim2, bool four, void* stream) {
-  if (!k || !v || !k_out || !v_out || batch < 0 || k_max < 0 || !idx || !count) return DUSTIN_ERR_INVALID_ARG;
-  if (!same_layout(k, v) || !same_layout(k_out, v_out) || k->num_kv_heads != k_out->num_kv_heads ||
+  if (!k || !k_out || !v != !v_out || batch < 0 || k_max < 0 || !idx || !count) return DUSTIN_ERR_INVALID_ARG;
+  if ((v && (!same_layout(k, v) || !same_layout(k_out, v_out))) || k->num_kv_heads != k_out->num_kv_heads ||
       k->head_dim != k_out->head_dim)
     return DUSTIN_ERR_INVALID_ARG;
   if (groups != 1 && groups != k->num_kv_heads) return DUSTIN_ERR_INVALID_ARG;
@@ -242,13 +242,14 @@ dustin_status evict(const Kv* k, const Kv* v, const Kv* k_out, const Kv* v_out, 
   EvictArgs a;
   memset(&a, 0, sizeof a);
   dustin_status st = evict_cache(k, 1, &a.src[0]);
-  if (st == DUSTIN_OK) st = evict_cache(v, 1, &a.src[1]);
+  if (st == DUSTIN_OK && v) st = evict_cache(v, 1, &a.src[1]);
   if (st == DUSTIN_OK) st = evict_cache(k_out, k_max, &a.dst[0]);
-  if (st == DUSTIN_OK) st = evict_cache(v_out, k_max, &a.dst[1]);
+  if (st == DUSTIN_OK && v) st = evict_cache(v_out, k_max, &a.dst[1]);
   if (st != DUSTIN_OK) return st;
   const bool same_k = same_cache(a.src[0], a.dst[0], k->num_kv_heads, batch);
-  const bool same_v = same_cache(a.src[1], a.dst[1], k->num_kv_heads, batch);
-  if (same_k != same_v || (!same_k && (k->data == k_out->data || v->data == v_out->data))) return DUSTIN_ERR_INVALID_ARG;
+  const bool same_v = v ? same_cache(a.src[1], a.dst[1], k->num_kv_heads, batch) : same_k;
+  if (same_k != same_v || (!same_k && (k->data == k_out->data || (v && v->data == v_out->data)))) return DUSTIN_ERR_INVALID_ARG;
+  a.caches = v ? 2 : 1;
   if (batch == 0) return DUSTIN_OK;
   a.idx = idx;
   a.idx_sb = idx_sb;

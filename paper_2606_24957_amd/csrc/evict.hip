@@ -62,8 +62,8 @@ __global__ __launch_bounds__(kEvictThreads) void evict_kernel(EvictArgs a, uint3
   const uint32_t part = blk - (uint32_t)b * parts;
   const uint32_t H = (uint32_t)a.num_kv_heads;
   const uint32_t e = part * kEvictThreads + threadIdx.x;
-  const uint32_t chunk = e % CPR, r = e / (2 * CPR);
-  const int is_v = (e / CPR) & 1;
+  const uint32_t chunk = e % CPR, r = a.caches == 2 ? e / (2 * CPR) : e / CPR;
+  const int is_v = a.caches == 2 ? (e / CPR) & 1 : 0;
   const uint32_t i = r / H, h = r - i * H;
   const int go = a.groups == 1 ? 0 : (int)h;
   if (i >= (uint32_t)clampi(a.count[b * a.groups + go], 0, a.k_max)) return;
@@ -93,8 +93,8 @@ __global__ __launch_bounds__(kEvictRunThreads) void evict_in_place_kernel(EvictA
   uint32_t blk = blockIdx.x - extra;
   const uint32_t slice = blk % slices;
   blk /= slices;
-  const int is_v = (int)(blk & 1);
-  blk >>= 1;
+  const int is_v = a.caches == 2 ? (int)(blk & 1) : 0;
+  blk /= (uint32_t)a.caches;
   const int b = (int)(blk / (uint32_t)a.num_kv_heads), h = (int)(blk % (uint32_t)a.num_kv_heads);
   const int go = a.groups == 1 ? 0 : h;
   const EvictCache& c = a.src[is_v];
@@ -150,14 +150,14 @@ hipError_t launch_evict(const EvictArgs& a, hipStream_t stream) {
   if (a.in_place) {
     const int sch = cpr < 4 ? cpr : 4;
     const int64_t slices = cpr / sch;
-    grid = extra + 2 * (int64_t)a.batch * a.num_kv_heads * slices;
+    grid = extra + a.caches * (int64_t)a.batch * a.num_kv_heads * slices;
     if (grid > INT32_MAX / kEvictRunThreads) return hipErrorInvalidValue;
     if (grid == 0) return hipSuccess;
     hipLaunchKernelGGL(sch == 4 ? evict_in_place_kernel<4> : evict_in_place_kernel<2>, dim3((unsigned)grid),
                        dim3(kEvictRunThreads), 0, stream, a, (uint32_t)slices, (uint32_t)extra);
     return hipGetLastError();
   }
-  const int64_t chunks = (int64_t)a.k_max * a.num_kv_heads * 2 * cpr;
+  const int64_t chunks = (int64_t)a.k_max * a.num_kv_heads * a.caches * cpr;
   const int64_t parts = (chunks + kEvictThreads - 1) / kEvictThreads;
   grid = extra + parts * a.batch;
   if (grid > INT32_MAX / kEvictThreads || chunks > INT32_MAX) return hipErrorInvalidValue;

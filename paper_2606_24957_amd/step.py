@@ -4,13 +4,19 @@ layers), the tiered top-k, and for every target layer the window's K/V append fo
 the sparse verification attention with the one index set (Sec. 3.2: a global, layer-invariant
 selection; accepted tokens are appended to the cache).  Every launch is a prepared libdustin
 call on one stream, so the whole step can be captured in a HIP graph and replayed.
+
+The layers' caches may be held in 4 bits (layer4); the scoring layer's keys then stay in bf16 beside them.  After a step,
+accept() verifies the drafted tokens against the target's logits and keeps the accepted ones, and evict() cuts every
+cache to the positions with the most accumulated attention.
 """
+import dataclasses
 from typing import List, Optional
 
 import torch
 
-from . import (digit_hist, plan_kv_append, plan_kv_commit, plan_score, plan_score_calls, plan_score_layers,
-               plan_score_per_layer, plan_sparse_verify_attn, plan_topk)
+from . import (KV4, digit_hist, kv4_append, kv4_empty, kv_evict, plan_kv4_append, plan_kv_append, plan_kv_commit,
+               plan_score, plan_score_calls, plan_score_layers, plan_score_per_layer, plan_sparse_verify_attn,
+               plan_sparse_verify_attn_kv4, plan_topk, topk, verify_tokens)
 
 
 def window_kv(s, layer) -> tuple:
@@ -27,12 +33,31 @@ def window_kv(s, layer) -> tuple:
     return k_new, v_new
 
 
+def layer4(s, layer):
+    """The layer with its caches in 4 bits: the rows that they hold, window included, appended to empty ones (in the
+    same pages)."""
+    kk, vv = layer.contiguous_kv(s)
+    B, n, paged = layer.k.shape[0], layer.k.shape[1], layer.page_table is not None
+    k, v = kv4_empty(B, n, s.num_kv_heads, s.head_dim, layer.k.device)
+    rows = [x + y for x, y in zip(s.seq_lens, s.n_query)]
+    T = max(rows)
+    kv4_append(kk[:, :T], vv[:, :T], k, v, [0] * s.B, n_query=rows, page_table=layer.page_table,
+               max_len=(layer.page_table.shape[1] * n if paged else n) - T)
+    return dataclasses.replace(layer, k=k, v=v)
+
+
 class VerifyStep:
     """The step's launches over fixed buffers: run() enqueues them eagerly, capture() records
-    them in a HIP graph and replay() launches the graph."""
+    them in a HIP graph and replay() launches the graph.  score_k: the scoring layer's keys in bf16, where the layers'
+    caches are held in 4 bits (their rows follow those of the first layer)."""
 
-    def __init__(self, s, layers, est, device, windows: Optional[list] = None, append: bool = True):
+    def __init__(self, s, layers, est, device, windows: Optional[list] = None, append: bool = True, score_k=None):
         self.s, self.layers, self.est, self.append = s, layers, est, append
+        self.score_k = layers[0].k if score_k is None else score_k
+        if isinstance(self.score_k, KV4):
+            raise ValueError("the scores read a bf16 cache: with 4-bit layers, give score_k")
+        if windows is None and isinstance(layers[0].k, KV4):
+            raise ValueError("with 4-bit layers, give the windows' K and V")
         i32 = lambda x: torch.tensor(list(x), dtype=torch.int32, device=device)
         self.seq, self.nq, self.gam = i32(s.seq_lens), i32(s.n_query), i32(s.draft_gamma)
         self.bud, self.mm = i32(s.budget), i32(s.m)
@@ -56,7 +81,7 @@ class VerifyStep:
         init = est.init_target
         if init is not None and s.groups > 1:  # one historical row, the same for every group
             init = init.expand(s.B, s.groups, N)
-        target = plan_score(est.q_target, self.layers[0].k, self.seq, s.target_heads, groups=s.groups,
+        target = plan_score(est.q_target, self.score_k, self.seq, s.target_heads, groups=s.groups,
                             init=init, out=self.s_t, max_len=N, page_table=self.layers[0].page_table,
                             stream=stream)
         if est.s_draft_given is not None:
@@ -71,13 +96,20 @@ class VerifyStep:
         ops.append(plan_topk(self.s_d, self.s_t, self.seq, s.k_max, budget=self.bud, m=self.mm,
                              n_sink=s.n_sink, n_window=s.n_window, groups=s.groups, idx=self.idx,
                              count=self.cnt, hist_d=self.hist_d, hist_t=self.hist_t, stream=stream))
+        if self.append and self.score_k is not self.layers[0].k:
+            k_new = self.windows[0][0]  # (keys alone: the append's two halves write the same rows)
+            ops.append(plan_kv_append(k_new, k_new, self.score_k, self.score_k, self.seq, n_query=self.nq,
+                                      page_table=self.layers[0].page_table, max_len=N, stream=stream))
         for L, o, (k_new, v_new) in zip(self.layers, self.outs, self.windows):
+            four = isinstance(L.k, KV4)
             if self.append:
-                ops.append(plan_kv_append(k_new, v_new, L.k, L.v, self.seq, n_query=self.nq,
-                                          page_table=L.page_table, max_len=N, stream=stream))
-            ops.append(plan_sparse_verify_attn(L.q, L.k, L.v, self.idx, self.cnt, self.seq,
-                                               n_query=self.nq, page_table=L.page_table, out=o,
-                                               stream=stream))
+                ops.append((plan_kv4_append if four else plan_kv_append)(
+                    k_new, v_new, L.k, L.v, self.seq, n_query=self.nq, page_table=L.page_table, max_len=N,
+                    stream=stream))
+            kw = dict(max_len=N) if four else {}
+            ops.append((plan_sparse_verify_attn_kv4 if four else plan_sparse_verify_attn)(
+                L.q, L.k, L.v, self.idx, self.cnt, self.seq, n_query=self.nq, page_table=L.page_table, out=o,
+                stream=stream, **kw))
         return ops
 
     def run(self):
@@ -108,6 +140,28 @@ class VerifyStep:
     def commit(self, accepted: torch.Tensor):
         """After verification: N_b += accepted_b (clamped to [0, T_b])."""
         plan_kv_commit(self.seq, accepted, n_query=self.nq, nq_max=self.s.t_max)()
+
+    def accept(self, logits, draft, u_accept, u, **kw):
+        """The drafted tokens against the target's logits [B, T_max, V] of the window (verify_tokens, with its settings):
+        keeps the accepted ones' rows; returns (accepted, token)."""
+        accepted, token = verify_tokens(logits, draft, u_accept, u, n_query=self.nq, **kw)
+        self.commit(accepted)
+        return accepted, token
+
+    def evict(self, weights: torch.Tensor, keep: int):
+        """Cuts every cache, in place, to the keep positions of each sequence with the largest weights (fp32
+        [B, 1, >= n_max], such as the accumulated target scores s_t), sinks and recent ones among them; the weights and
+        the lengths follow.  Returns (idx, count)."""
+        s, first = self.s, self.layers[0]
+        idx, cnt = topk(None, weights, self.seq, keep, n_sink=s.n_sink, n_window=s.n_window)
+        kv_evict(first.k, first.v, idx, cnt, page_table=first.page_table, weights=weights, new_lens=self.seq)
+        for L in self.layers[1:]:
+            kv_evict(L.k, L.v, idx, cnt, page_table=L.page_table)
+        if self.score_k is not first.k:
+            kv_evict(self.score_k, None, idx, cnt, page_table=first.page_table)
+        for k in self.est.draft_k:
+            kv_evict(k, None, idx, cnt)
+        return idx, cnt
 
 
 def draft_layer_of(layer: int, n_target: int, n_draft: int) -> int:

@@ -99,14 +99,13 @@ dustin_status kv4_rows(bool append, const void* k_rows, int64_t k_sb, int64_t k_
 
 // ---- attention
 
-constexpr int kAttn4Units = 256;
+constexpr int64_t kAttn4Units = 256;  // one to a CU: its LDS holds one
 constexpr int64_t kAttn4MaxPairs = 65536;
 
 // Workgroups of a call whose pairs hold up to `tokens` tokens, window included.
 int attn4_units(int64_t pairs, int64_t tokens) {
   const int64_t most = pairs * ((tokens + kAttn4Granule - 1) / kAttn4Granule);
-  const int64_t cap = env_int("DUSTIN_KV4_UNITS", kAttn4Units);
-  const int64_t u = most < cap ? most : cap;
+  const int64_t u = most < kAttn4Units ? most : kAttn4Units;
   return (int)((u + 7) / 8 * 8);
 }
 
@@ -131,7 +130,7 @@ dustin_status attn4(bool sparse, const void* q, int64_t q_sb, int64_t q_st, int6
   const int H = k->num_kv_heads;
   if (num_q_heads <= 0 || H <= 0 || num_q_heads % H || !same_layout(k, v)) return DUSTIN_ERR_INVALID_ARG;
   if (k->head_dim != 128) return DUSTIN_ERR_UNSUPPORTED;
-  if (bt->max_len > INT32_MAX - 1024) return DUSTIN_ERR_UNSUPPORTED;  // positions N_b + t are int32
+  if (bt->max_len > INT32_MAX - 4096) return DUSTIN_ERR_UNSUPPORTED;  // int32, with the rounds that are loaded ahead
   if (!rows_aligned(q, q_sb, q_st, q_sh) || !rows_aligned(out, o_sb, o_st, o_sh)) return DUSTIN_ERR_INVALID_ARG;
   const int gs = num_q_heads / H;
   if ((int64_t)bt->nq_max * gs > 128) return DUSTIN_ERR_UNSUPPORTED;
@@ -140,7 +139,7 @@ dustin_status attn4(bool sparse, const void* q, int64_t q_sb, int64_t q_st, int6
   if (sparse) {
     if (!idx || !count || (groups != 1 && groups != H)) return DUSTIN_ERR_INVALID_ARG;
     if (!aligned(idx, 4) || !aligned(count, 4) || idx_sb < 0 || idx_sg < 0) return DUSTIN_ERR_INVALID_ARG;
-    if (bt->k_max > INT32_MAX - 1024) return DUSTIN_ERR_UNSUPPORTED;
+    if (bt->k_max > INT32_MAX - 4096) return DUSTIN_ERR_UNSUPPORTED;
   }
   Attn4Args a;
   memset(&a, 0, sizeof a);
@@ -153,7 +152,7 @@ dustin_status attn4(bool sparse, const void* q, int64_t q_sb, int64_t q_st, int6
     for (const int64_t x : {c->stride_n, c->sstride_n, c->stride_page, c->sstride_page})
       if (x > (int64_t)UINT32_MAX) return DUSTIN_ERR_UNSUPPORTED;
   const int64_t tokens = (int64_t)(sparse ? bt->k_max : bt->max_len) + bt->nq_max;
-  if (pairs * ((tokens + kAttn4Granule - 1) / kAttn4Granule) > INT32_MAX) return DUSTIN_ERR_UNSUPPORTED;
+  if (pairs * ((tokens + kAttn4Granule - 1) / kAttn4Granule) > INT32_MAX / 2) return DUSTIN_ERR_UNSUPPORTED;
   if (bt->batch == 0 || bt->nq_max == 0) return DUSTIN_OK;
   a.q = static_cast<const uint16_t*>(q);
   a.q_sb = q_sb;
@@ -175,7 +174,6 @@ dustin_status attn4(bool sparse, const void* q, int64_t q_sb, int64_t q_st, int6
   a.scale_log2 = scale * kLog2e;
   a.rows_max = bt->nq_max * gs;
   a.units = attn4_units(pairs, tokens);
-  a.min_granules = 1;
   const Attn4Ws w = attn4_ws(pairs, a.units, a.rows_max);
   if (!ws || ws_bytes < w.total || !aligned(ws, kAlign)) return DUSTIN_ERR_WORKSPACE;
   char* base = static_cast<char*>(ws);

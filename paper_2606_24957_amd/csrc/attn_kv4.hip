@@ -60,14 +60,30 @@ __device__ __forceinline__ int read_word(uint32_t x) {
   asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(u) : "v"(x) : "memory");
   return u;
 }
+// The raw rows of a lane's token (K's and V's 16 bytes, their scale bytes), with n words of the rings.
 template <int n>
-__device__ __forceinline__ void read_words(const uint32_t (&x)[n], int (&u)[n]) {
-  if constexpr (n == 2)
-    asm volatile("ds_read_b32 %0, %2\n\tds_read_b32 %1, %3\n\ts_waitcnt lgkmcnt(0)"
-                 : "=&v"(u[0]), "=&v"(u[1]) : "v"(x[0]), "v"(x[1]) : "memory");
-  else
-    asm volatile("ds_read_b32 %0, %3\n\tds_read_b32 %1, %4\n\tds_read_b32 %2, %5\n\ts_waitcnt lgkmcnt(0)"
-                 : "=&v"(u[0]), "=&v"(u[1]), "=&v"(u[2]) : "v"(x[0]), "v"(x[1]), "v"(x[2]) : "memory");
+__device__ __forceinline__ void read_raw(uint32_t rows, uint32_t scales, const uint32_t (&at)[3], u32x4& kd, u32x4& vd,
+                                         uint32_t& kse, uint32_t& vse, int (&word)[3]) {
+  if constexpr (n == 0) {
+    asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:1024\n\tds_read_u8 %2, %5\n\t"
+                 "ds_read_u8 %3, %5 offset:64\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(kd), "=&v"(vd), "=&v"(kse), "=&v"(vse)
+                 : "v"(rows), "v"(scales)
+                 : "memory");
+  } else if constexpr (n == 1) {
+    asm volatile("ds_read_b128 %0, %5\n\tds_read_b128 %1, %5 offset:1024\n\tds_read_u8 %2, %6\n\t"
+                 "ds_read_u8 %3, %6 offset:64\n\tds_read_b32 %4, %7\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(kd), "=&v"(vd), "=&v"(kse), "=&v"(vse), "=&v"(word[0])
+                 : "v"(rows), "v"(scales), "v"(at[0])
+                 : "memory");
+  } else {
+    asm volatile("ds_read_b128 %0, %7\n\tds_read_b128 %1, %7 offset:1024\n\tds_read_u8 %2, %8\n\t"
+                 "ds_read_u8 %3, %8 offset:64\n\tds_read_b32 %4, %9\n\tds_read_b32 %5, %10\n\t"
+                 "ds_read_b32 %6, %11\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(kd), "=&v"(vd), "=&v"(kse), "=&v"(vse), "=&v"(word[0]), "=&v"(word[1]), "=&v"(word[2])
+                 : "v"(rows), "v"(scales), "v"(at[0]), "v"(at[1]), "v"(at[2])
+                 : "memory");
+  }
 }
 
 __device__ __forceinline__ u32x2 read_tr16(const char* p) {
@@ -116,17 +132,15 @@ __device__ __forceinline__ Pair4 pair_of(const Attn4Args& a, int pair) {
 }
 
 __device__ __forceinline__ int run_length(const Attn4Args& a, int total) {
-  const int per = (int)(((int64_t)total + a.units - 1) / a.units);
-  return per < a.min_granules ? a.min_granules : per;
+  return max(1, (int)(((int64_t)total + a.units - 1) / a.units));
 }
 
 template <int RT, bool kSparse, bool kPaged>
 __global__ __launch_bounds__(kThreads4) void attn_kv4_kernel(Attn4Args a) {
   constexpr int kTpw = 16;                       // tokens of a wave's round
-  constexpr int NT = kTpw / 16;
   constexpr int kTok = kW4 * kTpw;               // of a round
   constexpr int kRaw = kTpw * 136;               // a wave's rows and scales of a round as they come from memory
-  constexpr int kRawLoads = 2 * NT + 1;
+  constexpr int kRawLoads = 3;
   constexpr int kSlots = RT <= 4 ? 3 : 2;        // rounds in flight
   // Two V tiles and two sets of probabilities, so that a round's are written while others still read those of the round
   // before: one barrier a round (where LDS holds them).
@@ -248,55 +262,29 @@ __global__ __launch_bounds__(kThreads4) void attn_kv4_kernel(Attn4Args a) {
     auto position = [&](int v, int sel) {
       return clampi(v < wstart ? (kSparse ? sel : v) : N + (v - wstart), 0, cap_m1);
     };
-    auto load_page = [&](int n) {
+    auto load_page = [&](int n, int sel) {  // sel: the round's entry `lane` of the positions
       if constexpr (kPaged)
-        if (lane < kTpw) {
-          const int sel = kSparse ? read_word(lds_addr(pos_ring) + ring_of(n) + 4 * lane) : 0;
+        if (lane < kTpw)
           dma4(a.k.page_table + (int64_t)b * a.k.max_pages + (position(token(n, lane), sel) >> a.k.page_shift),
                page_ring + ring_of(n));
-        }
     };
     // (strides below 2^32: the host checks)
     auto offset = [&](int page, int slot, uint32_t sp, uint32_t sn) {
       const uint64_t o = (uint64_t)(uint32_t)slot * sn;
       return kPaged ? o + (uint64_t)(uint32_t)page * sp : o;
     };
-    auto load_rows = [&](int n, int slot_n) {
+    auto load_rows = [&](int n, int slot_n, int sel, int page) {  // sel, page: the round's entries lr
       char* const to = raw + slot_n * kRaw;
-      int j[NT + 1], page[NT + 1], slot[NT + 1];  // tokens of this lane's rows, and of its scale
-#pragma unroll
-      for (int i = 0; i < NT; ++i) j[i] = 16 * i + lr;
-      j[NT] = lane & (kTpw - 1);
-      int sel[NT + 1];
-      uint32_t at[NT + 1];
-#pragma unroll
-      for (int i = 0; i <= NT; ++i) sel[i] = page[i] = 0;
-      if constexpr (kSparse) {
-#pragma unroll
-        for (int i = 0; i <= NT; ++i) at[i] = lds_addr(pos_ring) + ring_of(n) + 4 * j[i];
-        read_words(at, sel);
-      }
+      int slot = position(token(n, lr), sel);
       if constexpr (kPaged) {
-#pragma unroll
-        for (int i = 0; i <= NT; ++i) at[i] = lds_addr(page_ring) + ring_of(n) + 4 * j[i];
-        read_words(at, page);
+        page = clampi(page, 0, a.k.num_pages - 1);
+        slot &= (1 << a.k.page_shift) - 1;
       }
-#pragma unroll
-      for (int i = 0; i <= NT; ++i) {
-        slot[i] = position(token(n, j[i]), sel[i]);
-        if constexpr (kPaged) {
-          page[i] = clampi(page[i], 0, a.k.num_pages - 1);
-          slot[i] &= (1 << a.k.page_shift) - 1;
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < NT; ++i) {
-        dma16(kdata + offset(page[i], slot[i], (uint32_t)a.k.stride_page, (uint32_t)a.k.stride_n), to + i * 1024);
-        dma16(vdata + offset(page[i], slot[i], (uint32_t)a.v.stride_page, (uint32_t)a.v.stride_n),
-              to + kTpw * 64 + i * 1024);
-      }
-      if (lane < 2 * kTpw) dma4(sdata + offset(page[NT], slot[NT], s_sp, s_sn), to + kTpw * 128);
+      dma16(kdata + offset(page, slot, (uint32_t)a.k.stride_page, (uint32_t)a.k.stride_n), to);
+      dma16(vdata + offset(page, slot, (uint32_t)a.v.stride_page, (uint32_t)a.v.stride_n), to + kTpw * 64);
+      if (lane < 2 * kTpw) dma4(sdata + offset(page, slot, s_sp, s_sn), to + kTpw * 128);
     };
+    const uint32_t pos_lane = lds_addr(pos_ring) + 4 * lr, page_lane = lds_addr(page_ring) + 4 * lr;
     if constexpr (kSparse) {
 #pragma unroll
       for (int n = 0; n < kSlots + 4; ++n) load_pos(n);
@@ -316,11 +304,12 @@ __global__ __launch_bounds__(kThreads4) void attn_kv4_kernel(Attn4Args a) {
     if constexpr (kSparse) wait_loads<0>();
     if constexpr (kPaged) {
 #pragma unroll
-      for (int n = 0; n < kSlots + 2; ++n) load_page(n);
+      for (int n = 0; n < kSlots + 2; ++n) load_page(n, kSparse ? read_word(pos_lane + ring_of(n)) : 0);
       wait_loads<0>();
     }
 #pragma unroll
-    for (int n = 0; n < kSlots; ++n) load_rows(n, n);
+    for (int n = 0; n < kSlots; ++n)
+      load_rows(n, n, kSparse ? read_word(pos_lane + ring_of(n)) : 0, kPaged ? read_word(page_lane + ring_of(n)) : 0);
     lds_barrier4();
     // (the first round's rows: no loads of positions or pages lie between it and those behind, as the loop's wait
     // counts them)
@@ -414,18 +403,17 @@ __global__ __launch_bounds__(kThreads4) void attn_kv4_kernel(Attn4Args a) {
         wait_loads<(kSlots - 1) * kRawLoads + kExtra>();
         u32x4 kd, vd;
         uint32_t kse, vse;
-        asm volatile(
-            "ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:1024\n\tds_read_u8 %2, %5\n\t"
-            "ds_read_u8 %3, %5 offset:64\n\ts_waitcnt lgkmcnt(0)"
-            : "=&v"(kd), "=&v"(vd), "=&v"(kse), "=&v"(vse)
-            : "v"(raw_lane + slot_n * kRaw), "v"(raw_scale + slot_n * kRaw)
-            : "memory");
+        const uint32_t at_sel = pos_lane + ring_of(n + kSlots), at_page = page_lane + ring_of(n + kSlots);
+        const uint32_t at[3] = {kSparse ? at_sel : at_page, at_page, pos_lane + ring_of(n + kSlots + 2)};
+        int word[3] = {0, 0, 0};
+        read_raw<kSparse && kPaged ? 3 : kExtra>(raw_lane + slot_n * kRaw, raw_scale + slot_n * kRaw, at, kd, vd, kse, vse,
+                                                 word);
 #pragma unroll
         for (int w = 0; w < 4; ++w)
           *reinterpret_cast<u32x4*>(v_at(set, wave * kTpw + lr, 4 * lg + w)) = kv4_decode8(vd[w], kv4_scale(vse));
         load_pos(n + kSlots + 4);
-        load_page(n + kSlots + 2);
-        load_rows(n + kSlots, slot_n);
+        load_page(n + kSlots + 2, word[2]);
+        load_rows(n + kSlots, slot_n, kSparse ? word[0] : 0, kSparse ? word[1] : word[0]);
         slot_n = slot_n + 1 == kSlots ? 0 : slot_n + 1;
 #pragma unroll
         for (int w = 0; w < 4; ++w) kop[w] = as_bf16x8(kv4_decode8(kd[w], kv4_scale(kse)));

@@ -114,7 +114,6 @@ struct Attn4Args {
   float scale_log2;
   int32_t idx_last;      // last entry of a selection's row
   int32_t units;         // runs at most, a multiple of 8
-  int32_t min_granules;  // smallest run of a workgroup
   int32_t rows_max;      // query rows of a KV head, at most
   float* part;           // [units][2][rows_max][128]
   float2* part_ml;       // [units][2][rows_max]

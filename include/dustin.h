@@ -540,10 +540,12 @@ dustin_status dustin_kv4_read(void* k_out, int64_t k_sb, int64_t k_st, int64_t k
  * dustin_sparse_verify_attn_kv4, dustin_dense_verify_attn_kv4 -- dustin_sparse_verify_attn and dense_verify_attn over
  * 4-bit caches of 128 channels: the same sums, with K and V the values that the caches stand for.  Arguments, limits
  * and rounding are theirs, but for
- *   - the caches' rows may lie anywhere a 64-bit offset reaches, pages need not be packed;
+ *   - the caches' rows may lie anywhere a 64-bit offset reaches, pages need not be packed; strides of positions and of
+ *     pages (data's and the scales') are below 2^32 bytes, and max_len and k_max at most 2^31 - 4097;
  *   - workspace: dustin_attn_kv4_workspace(...) bytes, 256-byte aligned, of any content.  Calls that share a
  *     workspace must not overlap.
- * max_tokens of the workspace is k_max (sparse) or max_len (dense).  batch * num_kv_heads <= 65536.
+ * max_tokens of the workspace is k_max (sparse) or max_len (dense).  batch * num_kv_heads <= 65536, and the granules of
+ * 128 tokens that max_tokens + nq_max come to, over all of them, at most 2^30.
  * --------------------------------------------------------------------------------- */
 size_t dustin_attn_kv4_workspace(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t nq_max,
                                  int32_t max_tokens);
@@ -572,9 +574,10 @@ dustin_status dustin_dense_verify_attn_kv4(const void* q, int64_t q_sb, int64_t 
  *       equal data, strides and page tables mark the call as in place.  Caches that overlap in another way are not
  *       supported, nor is one of K and V in place alone (DUSTIN_ERR_INVALID_ARG).  k_out and v_out address at least
  *       k_max positions.  v and v_out may be NULL (a cache of keys alone, as the scores read); one cache must not be
- *       given as both k and v.
+ *       given as both k and v, and a page that two sequences share must not be written.
  *   idx, count  int32 [B, groups, >= k_max] (strides idx_sb, idx_sg) and [B * groups]; ascending positions (in place,
- *       others give rows of unspecified content); groups 1 or the KV head count
+ *       others give rows of unspecified content); a position outside
+ *       the cache counts as its nearest end; groups 1 or the KV head count
  *   w, w_out    fp32 [B, groups, >= w_len], [B, groups, >= k_max] (strides in elements) or both NULL; w_out may be w
  *   new_lens    int32 [B] or NULL; may be the batch's seq_lens, which this call does not read
  * A step's layers share idx: pass w and new_lens with one of them.

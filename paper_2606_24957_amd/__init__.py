@@ -18,6 +18,7 @@ with the most accumulated attention (kv_evict).
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import os
 from typing import NamedTuple, Optional, Sequence, Tuple
@@ -872,6 +873,43 @@ def kv_commit(seq_lens, accepted, **kw):
 KV4_BLOCK = 32  # channels that share a scale
 
 
+def _planned(plan):
+    """What a plan function copies, converts or clears on the device, it does on the call's stream."""
+    @functools.wraps(plan)
+    def on_stream(*args, stream=None, **kw):
+        if stream is None:
+            return plan(*args, **kw)
+        with torch.cuda.stream(stream):
+            return plan(*args, stream=stream, **kw)
+    return on_stream
+
+
+def _on_device(*ts):
+    """The device of a call (under _planned: that of its stream) is the one its tensors are on."""
+    _on_gpu(*ts)
+    at = torch.cuda.current_device()
+    for t in ts:
+        if t is not None and t.device.index != at:
+            raise ValueError(f"a tensor is on {t.device}, the call's stream on device {at}")
+
+
+def _per_seq(x, B, device, name) -> Optional[torch.Tensor]:
+    """A per-sequence int32 array of at least B entries (or None)."""
+    x = _i32_dev(x, device)
+    if x is not None:
+        _on_device(x)
+        if x.numel() < B:
+            raise ValueError(f"{name} holds {x.numel()} of {B} sequences")
+    return x
+
+
+def _holds(B, cache, page_table):
+    """A cache (or its page table) holds B sequences."""
+    n = page_table.shape[0] if page_table is not None else cache.shape[0]
+    if n < B:
+        raise ValueError(f"the cache holds {n} of {B} sequences")
+
+
 class KV4(NamedTuple):
     """A K or V cache held in 4 bits (MXFP4; dustin_kv4): data uint8 [B, N_cap, Hkv, d / 2] (two channels a byte) and
     scales uint8 [B, N_cap, Hkv, d / 32], or [num_pages, page_size, Hkv, ...] with a page table."""
@@ -917,14 +955,14 @@ def kv4_view(cache: KV4, page_table: Optional[torch.Tensor] = None) -> DustinKV4
 
 def _kv4_pair(k: KV4, v: KV4, page_table) -> Tuple[DustinKV4, DustinKV4]:
     """The views of K and V, which share the page table (one copy of it if it is not contiguous)."""
-    _on_gpu(*k, *v, page_table)
+    _on_device(*k, *v, page_table)
     if page_table is not None:
         page_table = page_table.contiguous()
     return kv4_view(k, page_table), kv4_view(v, page_table)
 
 
 def _kv4_rows(fn, what, k_rows, v_rows, k, v, seq_lens, n_query, page_table, max_len, stream, result) -> Call:
-    _on_gpu(k_rows, v_rows)
+    _on_device(k_rows, v_rows)
     kv, vv = _kv4_pair(k, v, page_table)
     for t in (k_rows, v_rows):
         if t.dtype != torch.bfloat16 or t.dim() != 4 or t.stride(3) != 1:
@@ -932,17 +970,18 @@ def _kv4_rows(fn, what, k_rows, v_rows, k, v, seq_lens, n_query, page_table, max
         if t.shape != k_rows.shape or t.shape[2] != kv.num_kv_heads or t.shape[3] != kv.head_dim:
             raise ValueError(f"rows {tuple(t.shape)} do not fit caches of {kv.num_kv_heads} heads of {kv.head_dim}")
     B, nq_max = k_rows.shape[0], k_rows.shape[1]
-    if page_table is None and k.data.shape[0] < B:
-        raise ValueError("the cache holds fewer sequences than there are rows")
+    _holds(B, k.data, page_table)
+    _holds(B, v.data, page_table)
     dev = k_rows.device
     max_len = _capacity(kv) - nq_max if max_len is None else int(max_len)
-    seq, nqa = _i32_dev(seq_lens, dev), _i32_dev(n_query, dev)
+    seq, nqa = _per_seq(seq_lens, B, dev, "seq_lens"), _per_seq(n_query, B, dev, "n_query")
     bt = _batch(B, max_len, nq_max, 0, seq, nqa)
     args = (_ptr(k_rows), k_rows.stride(0), k_rows.stride(1), k_rows.stride(2), _ptr(v_rows), v_rows.stride(0),
             v_rows.stride(1), v_rows.stride(2), ctypes.byref(kv), ctypes.byref(vv), ctypes.byref(bt), _stream(stream))
     return Call(fn, args, what, (k_rows, v_rows, k, v, kv, vv, bt), result)
 
 
+@_planned
 def plan_kv4_append(k_new: torch.Tensor, v_new: torch.Tensor, k: KV4, v: KV4, seq_lens, *, n_query=None,
                     page_table: Optional[torch.Tensor] = None, max_len: Optional[int] = None, stream=None) -> Call:
     """Prepared dustin_kv4_append: k_new / v_new bf16 [B, T_max, Hkv, d] go, rounded into 4 bits, to positions
@@ -956,6 +995,7 @@ def kv4_append(k_new, v_new, k, v, seq_lens, **kw):
     return plan_kv4_append(k_new, v_new, k, v, seq_lens, **kw)()
 
 
+@_planned
 def plan_kv4_read(k: KV4, v: KV4, seq_lens, *, n_query=None, nq_max: Optional[int] = None,
                   page_table: Optional[torch.Tensor] = None, max_len: Optional[int] = None,
                   k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None, stream=None) -> Call:
@@ -980,20 +1020,22 @@ def kv4_read(k, v, seq_lens, **kw):
 
 
 def _plan_attn_kv4(q, k, v, idx, count, seq_lens, n_query, page_table, scale, out, max_len, stream) -> Call:
-    _on_gpu(q, out, idx, count)
+    _on_device(q, out, idx, count)
     kv, vv = _kv4_pair(k, v, page_table)
     if q.dtype != torch.bfloat16 or q.dim() != 4 or q.stride(3) != 1:
         raise ValueError("q must be bf16 [B, T, Hq, 128] with contiguous rows")
     B, nq_max, Hq, d = q.shape
-    if d != kv.head_dim or (page_table is None and k.data.shape[0] < B):
-        raise ValueError(f"q {tuple(q.shape)} does not fit the caches")
+    if d != kv.head_dim:
+        raise ValueError(f"q {tuple(q.shape)} does not fit caches of {kv.head_dim} channels")
+    _holds(B, k.data, page_table)
+    _holds(B, v.data, page_table)
     if out is None:
         out = torch.empty_like(q)
     if out.dtype != torch.bfloat16 or out.shape != q.shape or out.stride(3) != 1:
         raise ValueError("out must be bf16 of q's shape with contiguous rows")
     dev = q.device
     max_len = _capacity(kv) - nq_max if max_len is None else int(max_len)
-    seq, nqa = _i32_dev(seq_lens, dev), _i32_dev(n_query, dev)
+    seq, nqa = _per_seq(seq_lens, B, dev, "seq_lens"), _per_seq(n_query, B, dev, "n_query")
     scale = 1.0 / math.sqrt(d) if scale is None else scale
     k_max = 0 if idx is None else idx.shape[2]
     bt = _batch(B, max_len, nq_max, k_max, seq, nqa)
@@ -1017,6 +1059,7 @@ def _selection(idx, count, B):
     return count.contiguous()
 
 
+@_planned
 def plan_sparse_verify_attn_kv4(q: torch.Tensor, k: KV4, v: KV4, idx: torch.Tensor, count: torch.Tensor, seq_lens, *,
                                 n_query=None, page_table: Optional[torch.Tensor] = None,
                                 scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
@@ -1032,6 +1075,7 @@ def sparse_verify_attn_kv4(q, k, v, idx, count, seq_lens, **kw):
     return plan_sparse_verify_attn_kv4(q, k, v, idx, count, seq_lens, **kw)()
 
 
+@_planned
 def plan_dense_verify_attn_kv4(q: torch.Tensor, k: KV4, v: KV4, seq_lens, *, n_query=None,
                                page_table: Optional[torch.Tensor] = None, scale: Optional[float] = None,
                                out: Optional[torch.Tensor] = None, max_len: Optional[int] = None,
@@ -1047,14 +1091,15 @@ def dense_verify_attn_kv4(q, k, v, seq_lens, **kw):
 
 # ----------------------------------------------------------------------------- eviction
 
+@_planned
 def plan_kv_evict(k, v, idx: torch.Tensor, count: torch.Tensor, *, k_out=None, v_out=None,
                   page_table: Optional[torch.Tensor] = None, out_page_table: Optional[torch.Tensor] = None,
                   weights: Optional[torch.Tensor] = None, weights_out: Optional[torch.Tensor] = None,
                   new_lens: Optional[torch.Tensor] = None, stream=None) -> Call:
     """Prepared dustin_kv_evict (bf16 caches) or dustin_kv4_evict (KV4): a layer's rows idx[b, g, :count] to the front
     of k_out / v_out (with out_page_table), or of the caches themselves where no outputs are given.  v None: k alone
-    (a cache of keys that the scores read).  weights fp32
-    [B, G, N] go the same way into weights_out (None: in place), new_lens int32 [B] becomes the counts."""
+    (a cache of keys that the scores read).  weights fp32 [B, G, N] go the same way into weights_out (None: in place),
+    new_lens int32 [B] becomes the counts.  A page that two sequences share must not be written."""
     four = isinstance(k, KV4)
     if any(isinstance(x, KV4) != four for x in (v, k_out, v_out) if x is not None):
         raise ValueError("k, v, k_out and v_out are bf16 caches or KV4 caches")
@@ -1067,7 +1112,7 @@ def plan_kv_evict(k, v, idx: torch.Tensor, count: torch.Tensor, *, k_out=None, v
             raise ValueError("in place, the pages stay: out_page_table goes with outputs")
         k_out, v_out, out_page_table = k, v, page_table
     B, G, k_max = idx.shape
-    _on_gpu(idx, count, weights, weights_out, new_lens)
+    _on_device(idx, count, weights, weights_out, new_lens)
     count = _selection(idx, count, B)
     tables = [None if t is None else t.contiguous() for t in (page_table, out_page_table)]
     if page_table is out_page_table:
@@ -1075,12 +1120,12 @@ def plan_kv_evict(k, v, idx: torch.Tensor, count: torch.Tensor, *, k_out=None, v
     view, views = (kv4_view if four else kv_view), []
     for pair, t in zip(((k, v), (k_out, v_out)), tables):
         for x in pair:
-            _on_gpu(*(x if four and x is not None else (x,)), t)
-            views.append(None if x is None else view(x, t))
-    for x, t in zip((k, k_out), tables):
-        n = t.shape[0] if t is not None else (x.data if four else x).shape[0]
-        if n < B:
-            raise ValueError("the caches hold fewer sequences than idx")
+            if x is None:
+                views.append(None)
+                continue
+            _on_device(*(x if four else (x,)), t)
+            _holds(B, x.data if four else x, t)
+            views.append(view(x, t))
     if weights is None and weights_out is not None:
         raise ValueError("weights_out goes with weights")
     ws = (0, 0, 0, 0, 0)
@@ -1096,8 +1141,8 @@ def plan_kv_evict(k, v, idx: torch.Tensor, count: torch.Tensor, *, k_out=None, v
     if new_lens is not None and (new_lens.dtype != torch.int32 or new_lens.numel() < B or not new_lens.is_contiguous()):
         raise ValueError("new_lens must be a contiguous int32 [B] tensor")
     what = "dustin_kv4_evict" if four else "dustin_kv_evict"
-    args = (*(None if x is None else ctypes.byref(x) for x in views), B, _ptr(idx), idx.stride(0), idx.stride(1), _ptr(count), G, k_max,
-            _ptr(weights), ws[0], ws[1], ws[2], _ptr(weights_out), ws[3], ws[4], _ptr(new_lens), _stream(stream))
+    args = (*(None if x is None else ctypes.byref(x) for x in views), B, _ptr(idx), idx.stride(0), idx.stride(1),
+            _ptr(count), G, k_max, _ptr(weights), ws[0], ws[1], ws[2], _ptr(weights_out), ws[3], ws[4], _ptr(new_lens), _stream(stream))
     keep = (k, v, k_out, v_out, idx, count, tables, views, weights, weights_out, new_lens)
     return Call(getattr(lib(), what), args, what, keep, (k_out, v_out))
 
@@ -1119,7 +1164,7 @@ def _sampling(temperature, top_k, top_p, min_p, B, dev) -> DustinSampling:
     for name, x, dt in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
                         ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
         if isinstance(x, torch.Tensor):
-            _on_gpu(x)
+            _on_device(x)
             if x.dtype != dt or x.shape != (B,):
                 raise ValueError(f"{name} must be a number or a {dt} tensor [{B}]")
             x = x.contiguous()
@@ -1136,12 +1181,13 @@ def _vector(x, B, dt, name):
         raise ValueError(f"{name} must be a contiguous {dt} tensor [{B}]")
 
 
+@_planned
 def plan_sample(logits: torch.Tensor, u: torch.Tensor, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
                 token: Optional[torch.Tensor] = None, probs: Optional[torch.Tensor] = None, stream=None) -> Call:
     """Prepared dustin_sample: next tokens int32 [B] from logits bf16 or fp32 [B, V] and random numbers u fp32 [B] in
     [0, 1).  The settings are numbers or tensors [B].  With probs (fp32 [B, V]) the call also writes the distributions
     that the tokens are drawn from, and returns (token, probs)."""
-    _on_gpu(logits, u, token, probs)
+    _on_device(logits, u, token, probs)
     if logits.dtype not in _LOGITS or logits.dim() != 2 or (logits.stride(1) != 1 and logits.shape[1] > 1):
         raise ValueError("logits must be bf16 or fp32 [B, V] with contiguous rows")
     B, V = logits.shape
@@ -1167,6 +1213,7 @@ def sample(logits, u, **kw):
     return plan_sample(logits, u, **kw)()
 
 
+@_planned
 def plan_verify_tokens(logits: torch.Tensor, draft: torch.Tensor, u_accept: torch.Tensor, u: torch.Tensor, *,
                        draft_probs: Optional[torch.Tensor] = None, n_query=None, temperature=1.0, top_k=0, top_p=1.0,
                        min_p=0.0, accepted: Optional[torch.Tensor] = None, token: Optional[torch.Tensor] = None,
@@ -1174,7 +1221,7 @@ def plan_verify_tokens(logits: torch.Tensor, draft: torch.Tensor, u_accept: torc
     """Prepared dustin_verify_sample: logits bf16 or fp32 [B, T, V] of the window's tokens, draft int32 [B, T - 1],
     draft_probs fp32 [B, T - 1, V] (None: greedy drafts), random numbers u_accept fp32 [B, T - 1] and u fp32 [B].
     Returns (accepted, token) int32 [B]: the window tokens to keep, as kv_commit takes them, and the next token."""
-    _on_gpu(logits, draft, u_accept, u, draft_probs, accepted, token)
+    _on_device(logits, draft, u_accept, u, draft_probs, accepted, token)
     if logits.dtype not in _LOGITS or logits.dim() != 3 or (logits.stride(2) != 1 and logits.shape[2] > 1):
         raise ValueError("logits must be bf16 or fp32 [B, T, V] with contiguous rows")
     B, T, V = logits.shape
@@ -1190,9 +1237,7 @@ def plan_verify_tokens(logits: torch.Tensor, draft: torch.Tensor, u_accept: torc
     token = torch.empty(B, dtype=torch.int32, device=dev) if token is None else token
     _vector(accepted, B, torch.int32, "accepted")
     _vector(token, B, torch.int32, "token")
-    nqa = _i32_dev(n_query, dev)
-    if nqa is not None:
-        _vector(nqa, B, torch.int32, "n_query")
+    nqa = _per_seq(n_query, B, dev, "n_query")
     s = _sampling(temperature, top_k, top_p, min_p, B, dev)
     nbytes = lib().dustin_sample_workspace(B, T, V, dtype)
     ws = workspace(nbytes, dev, "sample", stream)

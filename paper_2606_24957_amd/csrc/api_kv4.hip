@@ -68,7 +68,9 @@ bool same_layout(const Kv* k, const Kv* v) {
 dustin_status kv4_rows(bool append, const void* k_rows, int64_t k_sb, int64_t k_st, int64_t k_sh, const void* v_rows,
                        int64_t v_sb, int64_t v_st, int64_t v_sh, const dustin_kv4* k, const dustin_kv4* v,
                        const dustin_batch* bt, void* stream) {
-  if (!batch_ok(bt) || !k_rows || !v_rows || !k || !v) return DUSTIN_ERR_INVALID_ARG;
+  if (!batch_ok(bt) || !k || !v) return DUSTIN_ERR_INVALID_ARG;
+  const bool none = bt->batch == 0 || bt->nq_max == 0;  // no rows: they may lie nowhere
+  if (!none && (!k_rows || !v_rows)) return DUSTIN_ERR_INVALID_ARG;
   if (!rows_aligned(k_rows, k_sb, k_st, k_sh) || !rows_aligned(v_rows, v_sb, v_st, v_sh)) return DUSTIN_ERR_INVALID_ARG;
   if (!same_layout(k, v)) return DUSTIN_ERR_INVALID_ARG;
   Kv4RowsArgs a;
@@ -78,6 +80,7 @@ dustin_status kv4_rows(bool append, const void* k_rows, int64_t k_sb, int64_t k_
   if (st == DUSTIN_OK) st = kv4_of(v, need, &a.v);
   if (st != DUSTIN_OK) return st;
   if ((int64_t)bt->nq_max * k->num_kv_heads * (k->head_dim / 8) > INT32_MAX / 4) return DUSTIN_ERR_UNSUPPORTED;
+  if (none) return DUSTIN_OK;
   a.k_in = static_cast<const uint16_t*>(k_rows);
   a.v_in = static_cast<const uint16_t*>(v_rows);
   a.k_out = const_cast<uint16_t*>(a.k_in);
@@ -125,7 +128,9 @@ dustin_status attn4(bool sparse, const void* q, int64_t q_sb, int64_t q_st, int6
                     const dustin_kv4* k, const dustin_kv4* v, const dustin_batch* bt, const int32_t* idx,
                     int64_t idx_sb, int64_t idx_sg, const int32_t* count, int32_t groups, float scale, void* out,
                     int64_t o_sb, int64_t o_st, int64_t o_sh, void* ws, size_t ws_bytes, void* stream) {
-  if (!batch_ok(bt) || !q || !out || !k || !v) return DUSTIN_ERR_INVALID_ARG;
+  if (!batch_ok(bt) || !k || !v) return DUSTIN_ERR_INVALID_ARG;
+  const bool none = bt->batch == 0 || bt->nq_max == 0;
+  if (!none && (!q || !out)) return DUSTIN_ERR_INVALID_ARG;
   if (!isfinite(scale) || !(scale > 0.f)) return DUSTIN_ERR_INVALID_ARG;
   const int H = k->num_kv_heads;
   if (num_q_heads <= 0 || H <= 0 || num_q_heads % H || !same_layout(k, v)) return DUSTIN_ERR_INVALID_ARG;
@@ -137,7 +142,8 @@ dustin_status attn4(bool sparse, const void* q, int64_t q_sb, int64_t q_st, int6
   const int64_t pairs = (int64_t)bt->batch * H;
   if (pairs > kAttn4MaxPairs) return DUSTIN_ERR_UNSUPPORTED;
   if (sparse) {
-    if (!idx || !count || (groups != 1 && groups != H)) return DUSTIN_ERR_INVALID_ARG;
+    if (!none && ((!idx && bt->k_max > 0) || !count)) return DUSTIN_ERR_INVALID_ARG;
+    if (groups != 1 && groups != H) return DUSTIN_ERR_INVALID_ARG;
     if (!aligned(idx, 4) || !aligned(count, 4) || idx_sb < 0 || idx_sg < 0) return DUSTIN_ERR_INVALID_ARG;
     if (bt->k_max > INT32_MAX - 4096) return DUSTIN_ERR_UNSUPPORTED;
   }
@@ -153,7 +159,7 @@ dustin_status attn4(bool sparse, const void* q, int64_t q_sb, int64_t q_st, int6
       if (x > (int64_t)UINT32_MAX) return DUSTIN_ERR_UNSUPPORTED;
   const int64_t tokens = (int64_t)(sparse ? bt->k_max : bt->max_len) + bt->nq_max;
   if (pairs * ((tokens + kAttn4Granule - 1) / kAttn4Granule) > INT32_MAX / 2) return DUSTIN_ERR_UNSUPPORTED;
-  if (bt->batch == 0 || bt->nq_max == 0) return DUSTIN_OK;
+  if (none) return DUSTIN_OK;
   a.q = static_cast<const uint16_t*>(q);
   a.q_sb = q_sb;
   a.q_st = q_st;
@@ -228,15 +234,18 @@ dustin_status evict(const Kv* k, const Kv* v, const Kv* k_out, const Kv* v_out, 
                     int64_t idx_sb, int64_t idx_sg, const int32_t* count, int32_t groups, int32_t k_max, const float* w,
                     int64_t w_sb, int64_t w_sg, int32_t w_len, float* w_out, int64_t wo_sb, int64_t wo_sg,
                     int32_t* new_lens, int row_bytes_per_dim2, bool four, void* stream) {
-  if (!k || !k_out || !v != !v_out || batch < 0 || k_max < 0 || !idx || !count) return DUSTIN_ERR_INVALID_ARG;
+  if (!k || !k_out || !v != !v_out || batch < 0 || k_max < 0) return DUSTIN_ERR_INVALID_ARG;
+  if (batch > 0 && ((!idx && k_max > 0) || !count)) return DUSTIN_ERR_INVALID_ARG;
   if ((v && (!same_layout(k, v) || !same_layout(k_out, v_out))) || k->num_kv_heads != k_out->num_kv_heads ||
       k->head_dim != k_out->head_dim)
     return DUSTIN_ERR_INVALID_ARG;
+  if (v && (k->data == v->data || k_out->data == v_out->data)) return DUSTIN_ERR_INVALID_ARG;
   if (groups != 1 && groups != k->num_kv_heads) return DUSTIN_ERR_INVALID_ARG;
   if (!aligned(idx, 4) || !aligned(count, 4) || !aligned(new_lens, 4) || idx_sb < 0 || idx_sg < 0)
     return DUSTIN_ERR_INVALID_ARG;
   if (!w != !w_out || !aligned(w, 4) || !aligned(w_out, 4)) return DUSTIN_ERR_INVALID_ARG;
   if (w && (w_len <= 0 || w_sb < 0 || w_sg < 0 || wo_sb < 0 || wo_sg < 0)) return DUSTIN_ERR_INVALID_ARG;
+  if (w && ((groups > 1 && wo_sg == 0) || (batch > 1 && wo_sb == 0))) return DUSTIN_ERR_INVALID_ARG;  // one row for several
   EvictArgs a;
   memset(&a, 0, sizeof a);
   dustin_status st = evict_cache(k, 1, &a.src[0]);

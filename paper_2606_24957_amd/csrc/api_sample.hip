@@ -48,7 +48,7 @@ SampleWs sample_ws(int64_t batch, int64_t rows, int64_t vocab, bool bf16) {
 
 dustin_status common(SampleArgs& a, const void* logits, int32_t dtype, int64_t sb, int64_t st, int32_t batch,
                      int32_t nq_max, int32_t vocab, const dustin_sampling* set, const float* u, int32_t* token) {
-  if (!logits || !set || !u || !token || batch < 0 || nq_max < 0 || vocab <= 0 || sb < 0 || st < 0)
+  if ((batch > 0 && (!logits || !u || !token)) || !set || batch < 0 || nq_max < 0 || vocab <= 0 || sb < 0 || st < 0)
     return DUSTIN_ERR_INVALID_ARG;
   if (dtype != DUSTIN_BF16 && dtype != DUSTIN_F32) return DUSTIN_ERR_INVALID_ARG;
   if (!aligned(logits, dtype == DUSTIN_BF16 ? 2 : 4) || !aligned(u, 4) || !aligned(token, 4) ||
@@ -137,9 +137,9 @@ dustin_status dustin_verify_sample(const void* logits, int32_t dtype, int64_t l_
   SampleArgs a;
   dustin_status st = common(a, logits, dtype, l_sb, l_st, batch, nq_max, vocab, set, u, token);
   if (st != DUSTIN_OK) return st;
-  if (!accepted || !aligned(accepted, 4) || !aligned(n_query, 4) || nq_max < 1) return DUSTIN_ERR_INVALID_ARG;
+  if ((batch > 0 && !accepted) || !aligned(accepted, 4) || !aligned(n_query, 4) || nq_max < 1) return DUSTIN_ERR_INVALID_ARG;
   if (nq_max > kSampleMaxWindow) return DUSTIN_ERR_UNSUPPORTED;
-  if (nq_max > 1 && (!draft || !u_accept || !aligned(draft, 4) || !aligned(u_accept, 4) || draft_sb < 0 || ua_sb < 0))
+  if (nq_max > 1 && ((batch > 0 && (!draft || !u_accept)) || !aligned(draft, 4) || !aligned(u_accept, 4) || draft_sb < 0 || ua_sb < 0))
     return DUSTIN_ERR_INVALID_ARG;
   if (draft_probs && (!aligned(draft_probs, 4) || q_sb < 0 || q_st < 0)) return DUSTIN_ERR_INVALID_ARG;
   if (batch == 0) return DUSTIN_OK;

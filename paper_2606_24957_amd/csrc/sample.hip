@@ -5,9 +5,8 @@
 // those the fewest whose weights reach top_p of the sum, of those the ones whose weight is at least min_p of the
 // largest.  It is described by the rank of its last token.  Three kernels:
 //   chunks  every workgroup takes a piece of a row: its largest logit, the sum of its weights against that, and where
-//           a filter needs it a histogram of counts and sums over eighths of octaves of the weight; the last one of a
-//           row joins these and finds the eighth in which the kept set ends
-//   rows    the tokens that have to be ranked are listed: all that may be kept where those are few (each is then
+//           a filter needs it a histogram of counts and sums over eighths of octaves of the weight
+//   rows    these joined, the eighth in which the kept set ends; the tokens that have to be ranked are listed: all that may be kept where those are few (each is then
 //           compared with each), otherwise those of the last eighth (ranked by histograms of ever finer ranges); where
 //           even these are many, one workgroup reads the row as often as it takes
 //   rest    (verification) what is left of the target's distribution after the first rejected draft, and the draw
@@ -51,6 +50,49 @@ struct Exp2 {
   }
 };
 
+// The same by a table, for the kernel that computes most weights: 2^d = 2^e 2^(j / 32) 2^r, |r| <= 1/64, and the Taylor
+// series of e^(r ln 2) to the 5th power (the next term is below 2^-48).  The table lies in LDS, an entry in two banks
+// of its own; it holds 2^(44 + j / 32), so that the result comes as a multiple of 2^-44.
+struct PowersOf2 {
+  double at[32];
+  constexpr PowersOf2() : at() {
+    for (int j = 0; j < 32; ++j) {
+      double t = 1.0, x = j * 0.693147180559945309417 / 32, sum = 0.0;
+      for (int i = 1; i < 24; ++i) {
+        sum += t;
+        t *= x / i;
+      }
+      at[j] = sum * 0x1p44;
+    }
+  }
+};
+__device__ constexpr PowersOf2 kPowers;
+struct TableExp2 {
+  double c[5];  // ln2^5 / 5! ... ln2
+  const double* table;
+  __device__ __forceinline__ explicit TableExp2(const double* lds) : table(lds) {
+    constexpr double l = 0.693147180559945309417;
+    const double x[5] = {l * l * l * l * l / 120, l * l * l * l / 24, l * l * l / 6, l * l / 2, l};
+#pragma unroll
+    for (int i = 0; i < 5; ++i) {
+      c[i] = x[i];
+      asm("" : "+s"(c[i]));
+    }
+  }
+  // 2^(44 + d) rounded to an integer, -46 <= d <= 0
+  __device__ __forceinline__ uint64_t units(double d) const {
+    const double t = __builtin_fma(d, 32.0, 0x1.8p52);  // (its low bits: 32 d as an integer)
+    const uint32_t k = (uint32_t)__double_as_longlong(t);
+    const double r = __builtin_fma(t - 0x1.8p52, -1.0 / 32, d);
+    double q = c[0];
+#pragma unroll
+    for (int i = 1; i < 5; ++i) q = __builtin_fma(q, r, c[i]);
+    q = __builtin_fma(q, r, 1.0);
+    const uint64_t u = (uint64_t)__double_as_longlong(table[k & 31]) + ((uint64_t)((k & ~31u) << 15) << 32);
+    return (uint64_t)__double_as_longlong(__builtin_fma(__longlong_as_double((long long)u), q, 0x1p52)) & 0xfffffffffffffull;
+  }
+};
+
 // A row's settings.
 struct Settings {
   bool greedy;
@@ -82,11 +124,13 @@ __device__ __forceinline__ double weight(const Exp2& exp2, float x, float top, d
   return w < 0x1p-45 ? 0.0 : w;
 }
 // ... as a multiple of 2^-44 (the mantissa bits of it + 2^52).  What lies below 2^-45.5 is rounded to zero.
-__device__ __forceinline__ uint64_t units_of(const Exp2& exp2, float x, float top, double scale) {
+__device__ __forceinline__ double exponent_of(float x, float top, double scale) {
   double d = ((double)x - (double)top) * scale;
   if (top == INFINITY) d = x == INFINITY ? 0.0 : -46.0;
-  d = d >= -46.0 ? d : -46.0;  // (and where x is NaN)
-  return (uint64_t)__double_as_longlong(exp2(d, kSampleFrac) + 0x1p52) & 0xfffffffffffffull;
+  return d >= -46.0 ? d : -46.0;  // (and where x is NaN)
+}
+__device__ __forceinline__ uint64_t units_of(const Exp2& exp2, float x, float top, double scale) {
+  return (uint64_t)__double_as_longlong(exp2(exponent_of(x, top, scale), kSampleFrac) + 0x1p52) & 0xfffffffffffffull;
 }
 
 __device__ __forceinline__ uint64_t rank_of(float x, int i) {
@@ -111,7 +155,7 @@ __device__ __forceinline__ uint64_t whole_key(uint32_t key) {
 }
 
 // Eighth of an octave that a logit's weight falls in (an integer, ascending with it).
-__device__ __forceinline__ double octave(float x, double scale) { return __builtin_floor((double)x * scale * 8.0); }
+__device__ __forceinline__ double octave(float x, double scale) { return __builtin_floor((double)x * (scale * 8.0)); }
 
 // The least key, of a row whose largest logit is top, whose logit satisfies a condition that holds from some logit on
 // (of top it does), near a guess of it.
@@ -195,21 +239,6 @@ struct RowReader {
   __device__ __forceinline__ static float of_bits(const u32x4& v, int e) {  // as it is (NaN stays NaN)
     if constexpr (kBf16) return __uint_as_float((e & 1) ? v[e / 2] & 0xffff0000u : v[e / 2] << 16);
     else return __uint_as_float(v[e]);
-  }
-  __device__ __forceinline__ void read(int g, float (&x)[n]) const {
-    const int i0 = first(g);
-    if (i0 >= 0 && i0 + n <= vocab) {
-      const u32x4 v = *reinterpret_cast<const u32x4*>(row + (int64_t)i0 * (kBf16 ? 2 : 4));
-#pragma unroll
-      for (int e = 0; e < n; ++e) {
-        if constexpr (kBf16) x[e] = __uint_as_float((e & 1) ? v[e / 2] & 0xffff0000u : v[e / 2] << 16);
-        else x[e] = __uint_as_float(v[e]);
-        if (x[e] != x[e]) x[e] = -INFINITY;
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < n; ++e) x[e] = i0 + e >= 0 && i0 + e < vocab ? at(i0 + e) : -INFINITY;
-    }
   }
 };
 
@@ -318,13 +347,15 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunk_kernel(SampleArgs 
   __shared__ unsigned long long sm_hist[kWaves][kSampleBins];
   __shared__ u32x4 sm_piece[kRowThreads];
   __shared__ uint64_t sm_red[kWaves];
+  __shared__ double sm_table[32];
   const int chunk = blockIdx.x, r = blockIdx.y, tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
   const int b = r / a.rows_per_seq, t = r - b * a.rows_per_seq;
   if (a.n_query && t >= a.n_query[b]) return;
   const RowReader<kBf16> row(a, b, t);
   const Settings s(a, b);
-  const Exp2 exp2;
   const bool filters = s.filters(), sums = !s.greedy && !s.counts_do();
+  if (tid < 32) sm_table[tid] = kPowers.at[tid];
+  const TableExp2 exp2(sm_table);
   if (filters)
     for (int i = lane; i < kSampleBins; i += kWave) sm_hist[wave][i] = 0;
   // the chunk's best token: its largest logit, then the lowest index that has it; the pieces wait in LDS
@@ -389,7 +420,7 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunk_kernel(SampleArgs 
       uint64_t w[n];
 #pragma unroll
       for (int e = 0; e < n; ++e) {
-        w[e] = sums ? units_of(exp2, row.of_bits(v, e), top, s.scale) : 0;
+        w[e] = sums ? exp2.units(exponent_of(row.of_bits(v, e), top, s.scale)) : 0;
         sum += w[e];
       }
       if (!filters) continue;

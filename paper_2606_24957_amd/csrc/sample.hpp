@@ -36,7 +36,7 @@ enum SampleMode : int32_t {
 struct SamplePlan {
   int32_t mode, bin;
   uint64_t lo, hi;          // ranks of the tokens to list
-  uint64_t before_cnt, before_sum;  // kRowList: tokens of better eighth of an octaves
+  uint64_t before_cnt, before_sum;  // kRowList: tokens of better eighths
   uint64_t all_sum;
   uint64_t least;           // rank of the last token that min_p keeps (~0: of any)
   double target;            // kRowList: running count or sum at which the last token is reached (negative: at `least`)

@@ -261,45 +261,51 @@ __device__ __forceinline__ uint64_t wave_scan(uint64_t x, uint64_t old, Op op) {
   x = dpp_step<0x142, 0xa>(x, old, op);  // the rows' last lanes to the rows behind
   return dpp_step<0x143, 0xc>(x, old, op);
 }
-__device__ __forceinline__ uint64_t last_lane(uint64_t x) {
-  return ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), kWave - 1) << 32) |
-         (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, kWave - 1);
+__device__ __forceinline__ uint64_t at_lane(uint64_t x, int lane) {  // (uniform lane)
+  return ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32) |
+         (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, lane);
 }
 __device__ __forceinline__ uint64_t wave_scan(uint64_t x) {
   return wave_scan(x, 0, [](uint64_t p, uint64_t q) { return p + q; });
 }
-__device__ __forceinline__ uint64_t wave_sum(uint64_t x) { return last_lane(wave_scan(x)); }
+__device__ __forceinline__ uint64_t wave_sum(uint64_t x) { return at_lane(wave_scan(x), kWave - 1); }
 __device__ __forceinline__ uint64_t wave_min(uint64_t x) {
-  return last_lane(wave_scan(x, ~0ull, [](uint64_t p, uint64_t q) { return q < p ? q : p; }));
+  return at_lane(wave_scan(x, ~0ull, [](uint64_t p, uint64_t q) { return q < p ? q : p; }), kWave - 1);
 }
 
-// Sum over a workgroup of `waves` waves, for every thread.
+// Inclusive sums over rows of 16 lanes.
+__device__ __forceinline__ uint64_t row_scan(uint64_t x) {
+  const auto add = [](uint64_t p, uint64_t q) { return p + q; };
+  x = dpp_step<0x111, 0xf>(x, 0, add);
+  x = dpp_step<0x112, 0xf>(x, 0, add);
+  x = dpp_step<0x114, 0xf>(x, 0, add);
+  return dpp_step<0x118, 0xf>(x, 0, add);
+}
+
+// Sum over a workgroup of `waves` waves, for every thread.  (The waves' sums are added up by a scan of 16 lanes: less
+// code than a loop over them, and most of what these kernels execute is fetched for the one time.)
 template <int waves>
 __device__ __forceinline__ uint64_t block_sum(uint64_t x, uint64_t* sm) {
-  x = wave_sum(x);
+  static_assert(waves <= 16, "a row of lanes");
+  const int lane = threadIdx.x & (kWave - 1);
+  x = wave_scan(x);
   __syncthreads();
-  if ((threadIdx.x & (kWave - 1)) == 0) sm[threadIdx.x / kWave] = x;
+  if (lane == kWave - 1) sm[threadIdx.x / kWave] = x;
   __syncthreads();
-  uint64_t s = 0;
-#pragma unroll
-  for (int w = 0; w < waves; ++w) s += sm[w];
-  return s;
+  return at_lane(row_scan(lane < waves ? sm[lane] : 0), waves - 1);
 }
 // The sums of the threads before this one, and of all.
 template <int waves>
 __device__ __forceinline__ uint64_t block_before(uint64_t x, uint64_t* sm, uint64_t& all) {
+  static_assert(waves <= 16, "a row of lanes");
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const uint64_t incl = wave_scan(x);
   __syncthreads();
-  if ((threadIdx.x & (kWave - 1)) == kWave - 1) sm[threadIdx.x / kWave] = incl;
+  if (lane == kWave - 1) sm[wave] = incl;
   __syncthreads();
-  uint64_t base = 0;
-  all = 0;
-#pragma unroll
-  for (int w = 0; w < waves; ++w) {
-    base += w < (int)threadIdx.x / kWave ? sm[w] : 0;
-    all += sm[w];
-  }
-  return base + incl - x;
+  const uint64_t own = lane < waves ? sm[lane] : 0, sums = row_scan(own);
+  all = at_lane(sums, waves - 1);
+  return at_lane(sums - own, wave) + incl - x;
 }
 
 // What a chunk's sums of weights are multiplied by to be against the row's largest logit.
@@ -318,21 +324,15 @@ struct Two {
 };
 template <int waves>
 __device__ __forceinline__ Two block_before(Two v, Two* sm, Two& all) {
+  static_assert(waves <= 16, "a row of lanes");
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const Two incl{wave_scan(v.x), wave_scan(v.y)};
   __syncthreads();
-  if ((threadIdx.x & (kWave - 1)) == kWave - 1) sm[threadIdx.x / kWave] = incl;
+  if (lane == kWave - 1) sm[wave] = incl;
   __syncthreads();
-  Two base{0, 0};
-  all = base;
-#pragma unroll
-  for (int w = 0; w < waves; ++w) {
-    const Two o = sm[w];
-    base.x += w < (int)threadIdx.x / kWave ? o.x : 0;
-    base.y += w < (int)threadIdx.x / kWave ? o.y : 0;
-    all.x += o.x;
-    all.y += o.y;
-  }
-  return {base.x + incl.x - v.x, base.y + incl.y - v.y};
+  const Two own = lane < waves ? sm[lane] : Two{0, 0}, sums{row_scan(own.x), row_scan(own.y)};
+  all = {at_lane(sums.x, waves - 1), at_lane(sums.y, waves - 1)};
+  return {at_lane(sums.x - own.x, wave) + incl.x - v.x, at_lane(sums.y - own.y, wave) + incl.y - v.y};
 }
 
 template <bool kBf16>

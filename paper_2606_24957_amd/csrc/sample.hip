@@ -79,17 +79,28 @@ struct TableExp2 {
       asm("" : "+s"(c[i]));
     }
   }
-  // 2^(44 + d) rounded to an integer, -46 <= d <= 0
-  __device__ __forceinline__ uint64_t units(double d) const {
+  // 2^(44 + d) = u q, -46 <= d <= 0
+  __device__ __forceinline__ double factors(double d, double& q) const {
     const double t = __builtin_fma(d, 32.0, 0x1.8p52);  // (its low bits: 32 d as an integer)
     const uint32_t k = (uint32_t)__double_as_longlong(t);
     const double r = __builtin_fma(t - 0x1.8p52, -1.0 / 32, d);
-    double q = c[0];
+    q = c[0];
 #pragma unroll
     for (int i = 1; i < 5; ++i) q = __builtin_fma(q, r, c[i]);
     q = __builtin_fma(q, r, 1.0);
     const uint64_t u = (uint64_t)__double_as_longlong(table[k & 31]) + ((uint64_t)((k & ~31u) << 15) << 32);
-    return (uint64_t)__double_as_longlong(__builtin_fma(__longlong_as_double((long long)u), q, 0x1p52)) & 0xfffffffffffffull;
+    return __longlong_as_double((long long)u);
+  }
+  __device__ __forceinline__ double operator()(double d) const {
+    double q;
+    const double u = factors(d, q);
+    return u * q;
+  }
+  // ... rounded to an integer
+  __device__ __forceinline__ uint64_t units(double d) const {
+    double q;
+    const double u = factors(d, q);
+    return (uint64_t)__double_as_longlong(__builtin_fma(u, q, 0x1p52)) & 0xfffffffffffffull;
   }
 };
 
@@ -335,6 +346,9 @@ __device__ __forceinline__ Two block_before(Two v, Two* sm, Two& all) {
   return {at_lane(sums.x - own.x, wave) + incl.x - v.x, at_lane(sums.y - own.y, wave) + incl.y - v.y};
 }
 
+// One read of the row: its tokens stay in LDS between the search for the largest and the weights against it.  Bound by
+// 64-bit arithmetic (13 operations a weight, 5 to its bin) and the LDS additions of the histogram: 128 rows of 151936
+// bf16 logits 31 us of mixed settings, 8 where only the largest is wanted (1.3 and 4.9 TB/s).
 template <bool kBf16>
 __global__ __launch_bounds__(kChunkThreads) void sample_chunk_kernel(SampleArgs a) {
   constexpr int n = RowReader<kBf16>::n, kMost = kRowThreads / kChunkThreads;  // pieces of a thread, at most
@@ -455,28 +469,38 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunk_kernel(SampleArgs 
     }
 }
 
-// Of the tokens of a chunk (one piece to a thread) with rank at most `last`, the one at which the running sum of
-// `value` passes `target` (the last with any, if none does); -1 where no token has any.
+// A piece that stays in registers; its tokens' logits one by one (-infinity outside the row).
+template <bool kBf16>
+struct Piece {
+  const RowReader<kBf16>& row;
+  int i0;
+  bool inside;
+  u32x4 bits;
+  __device__ __forceinline__ Piece(const RowReader<kBf16>& r, int g, bool is)
+      : row(r), i0(r.first(g)), inside(is && r.inside(g)), bits{0u, 0u, 0u, 0u} {
+    if (inside) bits = row.bits(g);
+  }
+  __device__ __forceinline__ float logit(int e) const {
+    constexpr int n = RowReader<kBf16>::n;
+    if (!inside) return i0 + e >= 0 && i0 + e < row.vocab ? row.at(i0 + e) : -INFINITY;
+    const int q = e * 4 / n;
+    const uint32_t y = q < 2 ? (q == 0 ? bits[0] : bits[1]) : (q == 2 ? bits[2] : bits[3]);
+    const float x = __uint_as_float(!kBf16 ? y : e & 1 ? y & 0xffff0000u : y << 16);
+    return x != x ? -INFINITY : x;
+  }
+};
+
+// Of the tokens of a chunk (one piece to a thread), the one at which the running sum of `value` passes `target` (the
+// last with any, if none does); -1 where no token has any.
 template <bool kBf16, class Value>
 __device__ int draw_in_chunk(const SampleArgs& a, const RowReader<kBf16>& row, int chunk, uint64_t target, Value value,
                              uint64_t* sm, int* sm_token) {
   constexpr int n = RowReader<kBf16>::n;
-  const int g = chunk * a.granules + (int)threadIdx.x, i0 = row.first(g);
-  const bool is = (int)threadIdx.x < a.granules, inside = is && row.inside(g);
-  u32x4 bits = {0u, 0u, 0u, 0u};
-  if (inside) bits = row.bits(g);
+  const bool is = (int)threadIdx.x < a.granules;
+  const Piece<kBf16> piece(row, chunk * a.granules + (int)threadIdx.x, is);
   auto at = [&](int e) -> uint64_t {
-    const int i = i0 + e;
-    float x;
-    if (inside) {
-      const int q = e * 4 / n;
-      const uint32_t y = q < 2 ? (q == 0 ? bits[0] : bits[1]) : (q == 2 ? bits[2] : bits[3]);
-      x = __uint_as_float(!kBf16 ? y : e & 1 ? y & 0xffff0000u : y << 16);
-    } else {
-      if (i < 0 || i >= a.vocab) return 0;
-      x = row.at(i);
-    }
-    return x == -INFINITY || x != x ? 0 : value(x, i);
+    const float x = piece.logit(e);
+    return x == -INFINITY ? 0 : value(x, piece.i0 + e);
   };
   uint64_t own = 0;
   if (is)
@@ -490,7 +514,7 @@ __device__ int draw_in_chunk(const SampleArgs& a, const RowReader<kBf16>& row, i
 #pragma unroll 1
     for (int e = 0; e < n; ++e) {
       const uint64_t v = at(e);
-      if (run <= target && target < run + v) *sm_token = i0 + e;
+      if (run <= target && target < run + v) *sm_token = piece.i0 + e;
       run += v;
     }
   __syncthreads();
@@ -515,8 +539,10 @@ __device__ int draw_chunk(const SampleArgs& a, float u, Value value, uint64_t* s
   return *sm_chunk;
 }
 
-// What the plan of a row leaves: up to `parts` workgroups list the tokens to be ranked, the last of them ranks them and
-// draws.
+// The chunks joined, and what is left to do planned (each of a row's workgroups does this for itself: handing a plan
+// over took longer); then up to `parts` workgroups list the tokens to be ranked, and the last of them ranks them and
+// draws.  Bound by latency: some twenty steps between barriers, and code that is executed once and fetched for it.  128
+// rows of 151936: 41 us, of which the second read of the rows is 7 to 10; one row of 32000: 15.
 template <bool kBf16, bool kDraw>
 __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
   constexpr int n = RowReader<kBf16>::n;
@@ -969,11 +995,18 @@ __global__ __launch_bounds__(kChunkThreads) void sample_probs_kernel(SampleArgs 
 }
 
 // A window's accepted drafts, and a chunk's share of the distribution that the next token is drawn from; the last
-// workgroup of a sequence draws it.
+// workgroup of a sequence draws it.  Bound by a chain of dependent reads (the rows' results, the drafts' logits, the
+// chunk, the others' sums, the chunk that holds the token) and, where nothing is filtered, by 64-bit arithmetic: 16
+// sequences of 151936 tokens with draft probabilities 21.4 us, one without 11.6 (weights by the 11th-power series over
+// the sum, and draft probabilities read one after another: 24.4 and 11.5).
 template <bool kBf16>
 __global__ __launch_bounds__(kRowThreads) void verify_rest_kernel(SampleArgs a) {
   constexpr int n = RowReader<kBf16>::n;
   __shared__ uint64_t sm_red[kRowWaves], sm_u64[2];
+  __shared__ Two sm_two[kRowWaves];
+  __shared__ SampleRow sm_row;
+  __shared__ double sm_table[32];
+  __shared__ float sm_q[kRowThreads * (n + 1)];
   __shared__ int sm_int[3];
   const int chunk = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
   const int T = a.n_query ? clampi(a.n_query[b], 0, a.rows_per_seq) : a.rows_per_seq;
@@ -986,12 +1019,15 @@ __global__ __launch_bounds__(kRowThreads) void verify_rest_kernel(SampleArgs a) 
     }
     return;
   }
+  if (tid >= kWave && tid < kWave + 32) sm_table[tid - kWave] = kPowers.at[tid - kWave];
   // ---- accepted drafts: draft t where u q(x) < p(x), up to the first that is not
   if (tid < kWave) {
     bool ok = false;
+    int x = -1;
+    SampleRow o{0, 0, 0.f};
+    if (tid < T) o = a.row[b * a.rows_per_seq + tid];
     if (tid < T - 1) {
-      const int x = a.draft[b * a.draft_sb + tid];
-      const SampleRow o = a.row[b * a.rows_per_seq + tid];
+      x = a.draft[b * a.draft_sb + tid];
       if (x >= 0 && x < a.vocab && o.sum) {
         const float l = RowReader<kBf16>(a, b, tid).at(x);
         const double p = l != -INFINITY && rank_of(l, x) <= o.last ? weight(exp2, l, o.top, s.scale) / ((double)o.sum * 0x1p-44) : 0.0;
@@ -999,49 +1035,70 @@ __global__ __launch_bounds__(kRowThreads) void verify_rest_kernel(SampleArgs a) 
         ok = (double)a.u_accept[b * a.ua_sb + tid] * q < p;
       }
     }
-    const uint64_t no = ~__ballot(ok);
-    if (tid == 0) sm_int[0] = min((int)__builtin_ctzll(no), T - 1);
+    const int first = min((int)__builtin_ctzll(~__ballot(ok)), T - 1);
+    if (tid == first) {
+      sm_int[0] = first;
+      sm_int[1] = x;
+      sm_row = o;
+    }
   }
   __syncthreads();
   const int kept = sm_int[0];
   const bool rejected = kept < T - 1;
   const RowReader<kBf16> row(a, b, kept);
-  const SampleRow o = a.row[b * a.rows_per_seq + kept];
-  const int x_draft = rejected ? a.draft[b * a.draft_sb + kept] : -1;
+  const SampleRow o = sm_row;
+  const int x_draft = sm_int[1];
   const float* q = rejected && a.q ? a.q + b * a.q_sb + kept * a.q_st : nullptr;
-  const double z = (double)o.sum * 0x1p-44;
-  // probabilities as multiples of 2^-60
+  const double z = 1.0 / (double)o.sum;
+  const TableExp2 power(sm_table);
+  // (a product with the sum's reciprocal: a bound of these rows is the rate of 64-bit arithmetic)
   auto whole = [&](float x, int i) -> double {
-    return rank_of(x, i) <= o.last ? weight(exp2, x, o.top, s.scale) / z : 0.0;
+    const double w = rank_of(x, i) <= o.last ? power(exponent_of(x, o.top, s.scale)) : 0.0;
+    return w < 0.5 ? 0.0 : w * z;
   };
-  auto rest = [&](double p, int i) {
-    if (rejected) p -= q ? (double)q[i] : i == x_draft ? 1.0 : 0.0;
+  // a thread's draft probabilities, all under way at once
+  float* const own_q = sm_q + tid * (n + 1);
+  auto fetch_q = [&](int i0) {
+    if (!q) return;
+    float x[n];
+    if (i0 >= 0 && i0 + n <= a.vocab) {
+#pragma unroll
+      for (int e = 0; e < n; ++e) x[e] = q[i0 + e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < n; ++e) x[e] = q[min(max(i0 + e, 0), a.vocab - 1)];
+    }
+#pragma unroll
+    for (int e = 0; e < n; ++e) own_q[e] = x[e];
+  };
+  auto rest = [&](double p, int i0, int e) {
+    if (rejected) p -= q ? (double)own_q[e] : i0 + e == x_draft ? 1.0 : 0.0;
     return p > 0.0 ? p : 0.0;
   };
+  // probabilities are summed as multiples of 2^-60
   auto fixed = [](double p) { return (uint64_t)__builtin_rint(p * 0x1p60); };
-  uint64_t r_sum = 0, p_sum = 0;
+  Two sum{0, 0};  // of what is left, and of the whole
   if (o.sum && tid < a.granules) {
-    const int i0 = row.first(chunk * a.granules + tid);
+    const Piece<kBf16> piece(row, chunk * a.granules + tid, true);
+    fetch_q(piece.i0);
     const float x_lo = bottom_of(o.last);
 #pragma unroll 1
     for (int e = 0; e < n; ++e) {
-      const int i = i0 + e;
-      if (i < 0 || i >= a.vocab) continue;
-      const float x = row.at(i);
+      const float x = piece.logit(e);
       if (x < x_lo || x == -INFINITY) continue;
-      const double p = whole(x, i);
+      const double p = whole(x, piece.i0 + e);
       if (p > 0.0) {
-        p_sum += fixed(p);
-        r_sum += fixed(rest(p, i));
+        sum.x += fixed(rest(p, piece.i0, e));
+        sum.y += fixed(p);
       }
     }
   }
-  r_sum = block_sum<kRowWaves>(r_sum, sm_red);
-  p_sum = block_sum<kRowWaves>(p_sum, sm_red);
+  Two sums;
+  block_before<kRowWaves>(sum, sm_two, sums);
   if (tid == 0) {
     uint64_t* at = a.r_sum + ((int64_t)b * a.chunks + chunk) * 2;
-    put(at, r_sum);
-    put(at + 1, p_sum);
+    put(at, sums.x);
+    put(at + 1, sums.y);
   }
   if (!arrive_last(&a.arrived[b], a.chunks, &sm_int[1])) return;
   if (tid == 0) a.accepted[b] = kept + 1;
@@ -1053,14 +1110,17 @@ __global__ __launch_bounds__(kRowThreads) void verify_rest_kernel(SampleArgs a) 
   __syncthreads();
   if (!of_rest) at = draw_chunk(a, u, [&](int c) { return stored(c, 1); }, sm_red, &sm_int[1], &sm_u64[0], all);
   int token = -1;
-  if (at >= 0)
+  if (at >= 0) {
+    const int i0 = row.first(at * a.granules + tid);
+    if (at != chunk && tid < a.granules) fetch_q(i0);
     token = draw_in_chunk<kBf16>(
         a, row, at, sm_u64[0],
         [&](float x, int i) {
           const double p = whole(x, i);
-          return p > 0.0 ? fixed(of_rest ? rest(p, i) : p) : 0;
+          return p > 0.0 ? fixed(of_rest ? rest(p, i0, i - i0) : p) : 0;
         },
         sm_red, &sm_int[2]);
+  }
   if (tid == 0) a.token[b] = token;
 }
 

@@ -639,7 +639,8 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
                                        [&](float x) { return weight(exp2, x, top, s.scale) >= s.m; }));
       const float x = logit_of_rank(plan.least);
       const int bin_m = x == top ? 0 : (int)(oct - octave(x, s.scale));
-      if (bin_m < bin) {
+      // (not where top_p is a part of the sum of the top_k: all of these are needed then)
+      if (bin_m < bin && !(count_scale && s.p < 1.0)) {
         bin = bin_m;
         target = -1.0;
       }

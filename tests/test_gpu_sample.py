@@ -222,3 +222,20 @@ def test_captured_and_replayed():
         torch.cuda.synchronize()
         check_window(x, draft, ua, u, q, nq, (1.0, 0, 0.9, 0.0), v.result)
         check(x[:, 0].double().cpu().numpy(), u.cpu().numpy(), ([1.0] * B, [40] * B, [1.0] * B, [0.0] * B), token=s.result)
+
+
+@pytest.mark.parametrize("kind", ["normal", "peaked", "few"])
+@pytest.mark.parametrize("V,dtype", [(5003, F), (40000, torch.bfloat16)])
+def test_all_filters_together(V, dtype, kind):
+    """Every filter with every other: what min_p leaves out still belongs to the sum that top_p is a part of."""
+    cols = list(zip(*[(t, k, p, m) for t in (1.0, 0.6) for k in (0, 20, 400, 700, 3000) for p in (1.0, 0.95, 0.6)
+                      for m in (0.0, 0.001, 0.05, 0.5)]))
+    B = len(cols[0])
+    x = torch.from_numpy(rows(kind, B, V, V + 1)).to(torch.float32).to(dtype).to(DEV)
+    u = torch.rand(B, generator=torch.Generator().manual_seed(V)).to(DEV)
+    kw = dict(temperature=torch.tensor(cols[0], device=DEV), top_k=torch.tensor(cols[1], dtype=torch.int32, device=DEV),
+              top_p=torch.tensor(cols[2], device=DEV), min_p=torch.tensor(cols[3], device=DEV))
+    probs = torch.full((B, V), float("nan"), device=DEV)
+    token, _ = D.sample(x, u, probs=probs, **kw)
+    torch.cuda.synchronize()
+    check(x.double().cpu().numpy(), u.cpu().numpy(), cols, probs.double().cpu().numpy(), token)

@@ -611,7 +611,8 @@ dustin_status dustin_kv4_evict(const dustin_kv4* k, const dustin_kv4* v, const d
  *   workspace  dustin_sample_workspace(batch, 1, vocab, dtype) bytes, 256-byte aligned.  Its first 512 KB must be zero
  *              before the first call; every call leaves them zero, so one buffer can serve calls of any shape.  Calls
  *              that share a workspace must not overlap.
- * Weights are computed in fp64 and summed as multiples of 2^-44: results do not depend on the order of the sums.
+ * Weights are computed in fp64 and summed as multiples of 2^-44 (of 2^-40 where the end of the kept set is sought):
+ * results do not depend on the order of the sums.
  *
  * dustin_verify_sample -- the drafted tokens of a verification window against the target's logits (speculative
  * sampling): the output is distributed as the target's own samples would be.  For every sequence b with T = T_b

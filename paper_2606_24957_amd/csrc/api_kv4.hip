@@ -102,7 +102,9 @@ dustin_status kv4_rows(bool append, const void* k_rows, int64_t k_sb, int64_t k_
 
 // ---- attention
 
-constexpr int64_t kAttn4Units = 256;  // one to a CU: its LDS holds one
+// Workgroups of a call: one to a CU, whose LDS holds one.  (128 pairs of 2053 tokens: 128 workgroups 41.3 us, 256 36.4;
+// more of them run one after another.)
+constexpr int64_t kAttn4Units = 256;
 constexpr int64_t kAttn4MaxPairs = 65536;
 
 // Workgroups of a call whose pairs hold up to `tokens` tokens, window included.

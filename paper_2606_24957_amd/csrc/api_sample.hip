@@ -11,22 +11,18 @@ namespace {
 
 constexpr int kMaxRows = 65535;  // rows of logits of a call: a dimension of the launch
 
-// Pieces of 16 bytes to a chunk, a power of two: 512, one to a thread, or 1024 where these fill the chip.
-int granules_of(int64_t rows, int64_t pieces) { return rows * ((pieces + 1023) / 1024) >= 512 ? 1024 : 512; }
-
 constexpr size_t kCounters = (kMaxRows + 1) * sizeof(uint32_t);  // of each kind
 
 // The workspace begins with the arrival and list counters, whatever a call's sizes are.
 struct SampleWs {
-  int granules, chunks;
+  int chunks;
   size_t row, list, c_top, c_best, c_sum, r_sum, h_cnt, h_sum, total;
 };
 
 SampleWs sample_ws(int64_t batch, int64_t rows, int64_t vocab, bool bf16) {
   SampleWs w;
   const int64_t pieces = vocab / (bf16 ? 8 : 4) + 2;  // a row may begin and end inside one
-  w.granules = granules_of(rows, pieces);
-  w.chunks = (int)((pieces + w.granules - 1) / w.granules);
+  w.chunks = (int)((pieces + kSamplePieces - 1) / kSamplePieces);
   size_t at = 2 * kCounters;
   auto take = [&](size_t bytes) {
     const size_t x = at;
@@ -83,7 +79,6 @@ dustin_status place(SampleArgs& a, bool bf16, void* ws, size_t ws_bytes) {
   const SampleWs w = sample_ws(a.batch, (int64_t)a.batch * a.rows_per_seq, a.vocab, bf16);
   if (!ws || ws_bytes < w.total || !aligned(ws, kAlign)) return DUSTIN_ERR_WORKSPACE;
   char* base = static_cast<char*>(ws);
-  a.granules = w.granules;
   a.chunks = w.chunks;
   a.arrived = reinterpret_cast<uint32_t*>(base);
   a.listed = reinterpret_cast<uint32_t*>(base + kCounters);

@@ -12,6 +12,15 @@
 //          product into LDS; and its tokens' V rows, decoded, into a tile that all waves share
 //   O      after the round's barrier each wave adds all the round's tokens to 16 of the 128 channels: O^T += V^T P^T
 // so that a wave holds an eighth of the accumulator, and nothing is left to add up at the end but the row sums.
+//
+// What it does not reach is memory's rate: a token is 136 bytes and, for each 16 query rows, 16 K multiply-adds, so
+// decoding, the value tile's way through LDS and the barrier of a round are in the way (vector unit 44 %, matrix unit
+// 27 %, LDS 40 % busy over a call).  Measured: 128 pairs of 2053 selected tokens and 40 rows 27.9 us and 4.7 for the
+// join (1.2 TB/s); the whole cache of 16 sequences of 4000 to 65536 tokens, 72 rows, pages of 16: 291 us (2.1 TB/s);
+// 16 pairs of 8192 tokens and 7 rows 11.6 and 3.9.  Other forms: two workgroups to a CU (one value tile, the queries
+// read from LDS, one round in flight) 26.7 for the first, 12.2 against 10.7 for the last; one value tile and two
+// barriers a round, 36 for the first with its join; every wave with tokens and an accumulator of its own, joined at the
+// end of a part, 46.
 #include "kv4.hpp"
 
 namespace dustin {
@@ -520,7 +529,8 @@ __global__ __launch_bounds__(kThreads4) void attn_kv4_kernel(Attn4Args a) {
 }
 
 // Joins the parts of a pair.  32 threads add up a query row's parts (four channels each), or every eighth of them where
-// a pair has many parts, of which a second step adds the eight sums; always in order.
+// a pair has many parts, of which a second step adds the eight sums; always in order.  (A kernel of its own: a last
+// workgroup of each pair that joins inside the first kernel would wait for the slowest of its parts.)
 template <bool kSparse, bool kMany>
 __global__ __launch_bounds__(256) void attn_kv4_merge_kernel(Attn4Args a) {
   __shared__ f32x4 sm_acc[kMany ? 8 : 1][32];
@@ -577,7 +587,7 @@ hipError_t launch_rt(const Attn4Args& a, int rt, hipStream_t stream) {
 #undef CASE
     default: return hipErrorInvalidValue;
   }
-  if (a.units > 8 * a.pairs)  // many parts to a pair
+  if (a.units > 8 * a.pairs)  // many parts to a pair (sixteen: 14.8 us for the call, without the second step 15.9)
     hipLaunchKernelGGL((attn_kv4_merge_kernel<kSparse, true>), dim3((unsigned)a.pairs, (unsigned)a.rows_max), dim3(256), 0,
                        stream, a);
   else

@@ -21,6 +21,7 @@ namespace {
 constexpr int kChunkThreads = 256;
 constexpr int kRowThreads = 1024;
 constexpr int kRowWaves = kRowThreads / kWave;
+static_assert(kSamplePieces == kRowThreads, "a piece to a thread");
 constexpr int kFew = kSampleFew, kList = kSampleList;
 constexpr int kPairs = 128;  // tokens that are compared each with each
 
@@ -378,29 +379,27 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunk_kernel(SampleArgs 
     u32x4 v[kMost];
 #pragma unroll
     for (int j = 0; j < kMost; ++j) {
-      const int g = chunk * a.granules + j * kChunkThreads + tid;
-      const bool is = j * kChunkThreads + tid < a.granules;
-      if (is && row.inside(g)) {
+      const int g = chunk * kSamplePieces + j * kChunkThreads + tid;
+      if (row.inside(g)) {
         v[j] = row.bits(g);
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[j][e] = kBf16 ? 0xff80ff80u : 0xff800000u;
-        if (is)
-          for (int e = 0; e < n; ++e) {  // the row's ends
-            const int i = row.first(g) + e;
-            if (i < 0 || i >= a.vocab) continue;
-            const uint32_t y = __float_as_uint(row.at(i));
-            if constexpr (kBf16) {
-              const uint32_t keep = e & 1 ? 0xffffu : 0xffff0000u;
+        for (int e = 0; e < n; ++e) {  // the row's ends
+          const int i = row.first(g) + e;
+          if (i < 0 || i >= a.vocab) continue;
+          const uint32_t y = __float_as_uint(row.at(i));
+          if constexpr (kBf16) {
+            const uint32_t keep = e & 1 ? 0xffffu : 0xffff0000u;
 #pragma unroll
-              for (int q = 0; q < 4; ++q)
-                if (e / 2 == q) v[j][q] = (v[j][q] & keep) | (e & 1 ? y : y >> 16);
-            } else {
+            for (int q = 0; q < 4; ++q)
+              if (e / 2 == q) v[j][q] = (v[j][q] & keep) | (e & 1 ? y : y >> 16);
+          } else {
 #pragma unroll
-              for (int q = 0; q < 4; ++q)
-                if (e == q) v[j][q] = y;
-            }
+            for (int q = 0; q < 4; ++q)
+              if (e == q) v[j][q] = y;
           }
+        }
       }
     }
     float big = -INFINITY;
@@ -416,7 +415,7 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunk_kernel(SampleArgs 
 #pragma unroll
         for (int e = n - 1; e >= 0; --e)
           if (row.of_bits(v[j], e) == big)
-            best = rank_of(big, row.first(chunk * a.granules + j * kChunkThreads + tid) + e);
+            best = rank_of(big, row.first(chunk * kSamplePieces + j * kChunkThreads + tid) + e);
     }
   }
   best = wave_min(best);
@@ -476,8 +475,8 @@ struct Piece {
   int i0;
   bool inside;
   u32x4 bits;
-  __device__ __forceinline__ Piece(const RowReader<kBf16>& r, int g, bool is)
-      : row(r), i0(r.first(g)), inside(is && r.inside(g)), bits{0u, 0u, 0u, 0u} {
+  __device__ __forceinline__ Piece(const RowReader<kBf16>& r, int g)
+      : row(r), i0(r.first(g)), inside(r.inside(g)), bits{0u, 0u, 0u, 0u} {
     if (inside) bits = row.bits(g);
   }
   __device__ __forceinline__ float logit(int e) const {
@@ -496,16 +495,14 @@ template <bool kBf16, class Value>
 __device__ int draw_in_chunk(const SampleArgs& a, const RowReader<kBf16>& row, int chunk, uint64_t target, Value value,
                              uint64_t* sm, int* sm_token) {
   constexpr int n = RowReader<kBf16>::n;
-  const bool is = (int)threadIdx.x < a.granules;
-  const Piece<kBf16> piece(row, chunk * a.granules + (int)threadIdx.x, is);
+  const Piece<kBf16> piece(row, chunk * kSamplePieces + (int)threadIdx.x);
   auto at = [&](int e) -> uint64_t {
     const float x = piece.logit(e);
     return x == -INFINITY ? 0 : value(x, piece.i0 + e);
   };
   uint64_t own = 0;
-  if (is)
 #pragma unroll 1
-    for (int e = 0; e < n; ++e) own += at(e);
+  for (int e = 0; e < n; ++e) own += at(e);
   if (threadIdx.x == 0) *sm_token = -1;
   uint64_t all;
   uint64_t run = block_before<kRowWaves>(own, sm, all);
@@ -564,7 +561,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
   const Settings s(a, b);
   const Exp2 exp2;
   const int64_t c0 = (int64_t)r * a.chunks;
-  const int pieces = a.granules * a.chunks;
+  const int pieces = kSamplePieces * a.chunks;
   const bool filters = s.filters(), sums = !s.greedy && !s.counts_do();
 
   // ---- the chunks joined: the row's best token, the sum of its weights, its histogram
@@ -628,7 +625,8 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
     // the eighth of an octave in which the kept set ends, by count or sum, and by min_p
     const bool by_count = s.k > 0 && (uint64_t)s.k < all.x;
     const bool count_scale = by_count || s.counts_do();
-    double target = by_count ? (double)s.k : s.counts_do() ? (double)all.x : s.p * (double)all_sum;
+    // (without top_k or top_p it ends nowhere; the sums, multiples of 2^-40 here, may be reached before the last token)
+    double target = by_count ? (double)s.k : s.counts_do() ? (double)all.x : s.p < 1.0 ? s.p * (double)all_sum : INFINITY;
     const double from = (double)(count_scale ? before.x : before.y);
     const double upto = (double)(count_scale ? before.x + my_cnt : before.y + my_sum);
     if (my_cnt && upto >= target && (from < target || tid == 0)) sm_int[0] = tid;  // one thread, or none
@@ -945,7 +943,8 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
   __syncthreads();
   if (plan.mode != kRowWhole && tid < a.chunks) sm_chunk_sum[tid] = 0;
   __syncthreads();
-  const int chunk_bits = 31 - __clz(a.granules * n);
+  constexpr int chunk_bits = 10 + (kBf16 ? 3 : 2);
+  static_assert(1 << chunk_bits == kSamplePieces * n, "tokens of a chunk");
   if (plan.mode == kRowList) {  // (a list with all that may be kept returned above)
     for (int c = tid / kWave; c < a.chunks; c += kRowWaves) {
       uint64_t x = 0;
@@ -1079,8 +1078,8 @@ __global__ __launch_bounds__(kRowThreads) void verify_rest_kernel(SampleArgs a) 
   // probabilities are summed as multiples of 2^-60
   auto fixed = [](double p) { return (uint64_t)__builtin_rint(p * 0x1p60); };
   Two sum{0, 0};  // of what is left, and of the whole
-  if (o.sum && tid < a.granules) {
-    const Piece<kBf16> piece(row, chunk * a.granules + tid, true);
+  if (o.sum) {
+    const Piece<kBf16> piece(row, chunk * kSamplePieces + tid);
     fetch_q(piece.i0);
     const float x_lo = bottom_of(o.last);
 #pragma unroll 1
@@ -1112,8 +1111,8 @@ __global__ __launch_bounds__(kRowThreads) void verify_rest_kernel(SampleArgs a) 
   if (!of_rest) at = draw_chunk(a, u, [&](int c) { return stored(c, 1); }, sm_red, &sm_int[1], &sm_u64[0], all);
   int token = -1;
   if (at >= 0) {
-    const int i0 = row.first(at * a.granules + tid);
-    if (at != chunk && tid < a.granules) fetch_q(i0);
+    const int i0 = row.first(at * kSamplePieces + tid);
+    if (at != chunk) fetch_q(i0);
     token = draw_in_chunk<kBf16>(
         a, row, at, sm_u64[0],
         [&](float x, int i) {

@@ -18,7 +18,8 @@ constexpr int kSampleBins = 368;     // eighths of octaves from the largest weig
 constexpr int kSampleFew = 1024;     // tokens ranked by comparing each with each
 constexpr int kSampleList = 4096;    // tokens of a list
 constexpr int kSampleMaxWindow = 64; // tokens of a verification window
-constexpr int kSampleMaxChunks = 136;  // 2^18 fp32 logits in chunks of 512 pieces, wherever the row begins
+constexpr int kSamplePieces = 1024;  // 16-byte pieces of a chunk of a row (with 512, 128 rows took 90 us for 72, one 24)
+constexpr int kSampleMaxChunks = 65;  // 2^18 fp32 logits, wherever the row begins
 
 struct SampleRow {  // what is known of a row once its filters are resolved
   uint64_t last;    // rank of the last kept token (0: none is)
@@ -66,8 +67,8 @@ struct SampleArgs {
   const float* u_accept;
   int64_t ua_sb;
   int32_t* accepted;
-  // chunks of `granules` 16-byte pieces, `chunks` to a row, and what is kept of them
-  int32_t granules, chunks;
+  // chunks of a row, and what is kept of them
+  int32_t chunks;
   float* c_top;       // [rows][chunks] largest logit
   uint64_t* c_best;   // best rank
   uint64_t* c_sum;    // sum of weights, against the chunk's largest

@@ -239,3 +239,19 @@ def test_all_filters_together(V, dtype, kind):
     token, _ = D.sample(x, u, probs=probs, **kw)
     torch.cuda.synchronize()
     check(x.double().cpu().numpy(), u.cpu().numpy(), cols, probs.double().cpu().numpy(), token)
+
+
+@pytest.mark.parametrize("V,dtype", [(300, F), (9001, F), (32000, torch.bfloat16)])
+def test_small_weights_stay_where_nothing_ends_the_set(V, dtype):
+    """A top_k beyond the tokens that have a weight keeps them all, down to 2^-45 of the largest."""
+    x = np.full((6, V), -1e30)
+    at = np.random.default_rng(V).permutation(V)[:120]
+    x[:, at] = -np.arange(120) * 0.25  # weights to e^-29.75 = 2^-42.9
+    x[3:, at] *= 1.04                  # to 2^-44.6
+    x = torch.from_numpy(x).to(torch.float32).to(dtype).to(DEV)
+    u = torch.tensor([0.0, 0.5, 1.0 - 2.0 ** -24] * 2, device=DEV)
+    cols = ([1.0] * 6, [V - 1] * 6, [1.0] * 6, [0.0] * 6)
+    probs = torch.full((6, V), float("nan"), device=DEV)
+    token, _ = D.sample(x, u, top_k=V - 1, probs=probs)
+    torch.cuda.synchronize()
+    check(x.double().cpu().numpy(), u.cpu().numpy(), cols, probs.double().cpu().numpy(), token)

@@ -46,10 +46,16 @@ def layer4(s, layer):
     return dataclasses.replace(layer, k=k, v=v)
 
 
+def _plan_sparse(layer):
+    """The sparse attention of the layer's kind of cache."""
+    return plan_sparse_verify_attn_kv4 if isinstance(layer.k, KV4) else plan_sparse_verify_attn
+
+
 class VerifyStep:
     """The step's launches over fixed buffers: run() enqueues them eagerly, capture() records
     them in a HIP graph and replay() launches the graph.  score_k: the scoring layer's keys in bf16, where the layers'
-    caches are held in 4 bits (their rows follow those of the first layer)."""
+    caches are held in 4 bits (their rows follow those of the first layer).  The calls are planned for lengths of up to
+    s.n_max before the window: once accepted tokens lead past it, evict() or plan a new step."""
 
     def __init__(self, s, layers, est, device, windows: Optional[list] = None, append: bool = True, score_k=None):
         self.s, self.layers, self.est, self.append = s, layers, est, append
@@ -101,15 +107,12 @@ class VerifyStep:
             ops.append(plan_kv_append(k_new, k_new, self.score_k, self.score_k, self.seq, n_query=self.nq,
                                       page_table=self.layers[0].page_table, max_len=N, stream=stream))
         for L, o, (k_new, v_new) in zip(self.layers, self.outs, self.windows):
-            four = isinstance(L.k, KV4)
             if self.append:
-                ops.append((plan_kv4_append if four else plan_kv_append)(
+                ops.append((plan_kv4_append if isinstance(L.k, KV4) else plan_kv_append)(
                     k_new, v_new, L.k, L.v, self.seq, n_query=self.nq, page_table=L.page_table, max_len=N,
                     stream=stream))
-            kw = dict(max_len=N) if four else {}
-            ops.append((plan_sparse_verify_attn_kv4 if four else plan_sparse_verify_attn)(
-                L.q, L.k, L.v, self.idx, self.cnt, self.seq, n_query=self.nq, page_table=L.page_table, out=o,
-                stream=stream, **kw))
+            ops.append(_plan_sparse(L)(L.q, L.k, L.v, self.idx, self.cnt, self.seq, n_query=self.nq,
+                                       page_table=L.page_table, out=o, stream=stream))
         return ops
 
     def run(self):
@@ -205,9 +208,9 @@ class PerLayerSelectionStep:
                              idx=self.idx, count=self.cnt))
         for i, (L, o) in enumerate(zip(self.layers, self.outs)):
             j = draft_layer_of(i, self.n_target, self.n_draft)
-            ops.append(plan_sparse_verify_attn(L.q, L.k, L.v, self.idx[j * B:(j + 1) * B],
-                                               self.cnt[j * B:(j + 1) * B], self.seq, n_query=self.nq,
-                                               page_table=L.page_table, out=o))
+            ops.append(_plan_sparse(L)(L.q, L.k, L.v, self.idx[j * B:(j + 1) * B],
+                                       self.cnt[j * B:(j + 1) * B], self.seq, n_query=self.nq,
+                                       page_table=L.page_table, out=o))
         return ops
 
     def run(self):

@@ -143,3 +143,26 @@ def test_4_bit_layers_need_a_scoring_cache():
     four = [S.layer4(s, l) for l in layers]
     with pytest.raises(ValueError, match="score_k"):
         S.VerifyStep(s, four, est, DEV, windows=[S.window_kv(s, l) for l in layers])
+
+
+def test_per_layer_selection_over_4_bits():
+    """The per-layer step selects by the draft model alone: the sets of the bf16 step, and the 4-bit attention over them."""
+    s = W.config("qwen7b").replace(B=2, seq_lens=(2000, 700), n_query=(5, 5), budget=(256, 256), m=(118, 118),
+                                   planted=(20,), layers=2, draft=W.DraftShape(layers=4))
+    layers = [W.make_layer(s, l, DEV) for l in range(s.layers)]
+    est = W.make_estimation(s, layers[0], DEV)
+    four = [S.layer4(s, l) for l in layers]
+    st16 = S.PerLayerSelectionStep(s, layers, est, DEV, n_target=8)
+    st4 = S.PerLayerSelectionStep(s, four, est, DEV, n_target=8)
+    st16.run()
+    st4.run()
+    torch.cuda.synchronize()
+    B = s.B
+    assert torch.equal(st4.cnt, st16.cnt)
+    for r in range(4 * B):
+        assert torch.equal(st4.idx[r, 0, :int(st4.cnt[r, 0])], st16.idx[r, 0, :int(st4.cnt[r, 0])])
+    for i, L in enumerate(four):
+        j = S.draft_layer_of(i, 8, 4)
+        ref = D.sparse_verify_attn_kv4(L.q, L.k, L.v, st4.idx[j * B:(j + 1) * B], st4.cnt[j * B:(j + 1) * B], st4.seq)
+        torch.cuda.synchronize()
+        assert torch.equal(st4.outs[i].view(torch.int16), ref.view(torch.int16))

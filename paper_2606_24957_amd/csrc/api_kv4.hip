@@ -102,15 +102,14 @@ dustin_status kv4_rows(bool append, const void* k_rows, int64_t k_sb, int64_t k_
 
 // ---- attention
 
-// Workgroups of a call: one to a CU, whose LDS holds one.  (128 pairs of 2053 tokens: 128 workgroups 41.3 us, 256 36.4;
-// more of them run one after another.)
-constexpr int64_t kAttn4Units = 256;
 constexpr int64_t kAttn4MaxPairs = 65536;
 
-// Workgroups of a call whose pairs hold up to `tokens` tokens, window included.
-int attn4_units(int64_t pairs, int64_t tokens) {
+// Workgroups of a call whose pairs hold up to `tokens` tokens, window included, and `rows` query rows: as many as run
+// at once.
+int attn4_units(int64_t pairs, int64_t tokens, int64_t rows) {
   const int64_t most = pairs * ((tokens + kAttn4Granule - 1) / kAttn4Granule);
-  const int64_t u = most < kAttn4Units ? most : kAttn4Units;
+  const int64_t cap = rows <= 16 * kAttn4Two ? 2 * kAttn4Cus : kAttn4Cus;
+  const int64_t u = most < cap ? most : cap;
   return (int)((u + 7) / 8 * 8);
 }
 
@@ -181,7 +180,7 @@ dustin_status attn4(bool sparse, const void* q, int64_t q_sb, int64_t q_st, int6
   a.pairs = (int32_t)pairs;
   a.scale_log2 = scale * kLog2e;
   a.rows_max = bt->nq_max * gs;
-  a.units = attn4_units(pairs, tokens);
+  a.units = attn4_units(pairs, tokens, a.rows_max);
   const Attn4Ws w = attn4_ws(pairs, a.units, a.rows_max);
   if (!ws || ws_bytes < w.total || !aligned(ws, kAlign)) return DUSTIN_ERR_WORKSPACE;
   char* base = static_cast<char*>(ws);
@@ -303,7 +302,8 @@ size_t dustin_attn_kv4_workspace(int32_t batch, int32_t num_q_heads, int32_t num
   if (batch <= 0 || num_kv_heads <= 0 || num_q_heads <= 0 || num_q_heads % num_kv_heads || nq_max <= 0 || max_tokens < 0)
     return 0;
   const int64_t pairs = (int64_t)batch * num_kv_heads;
-  return attn4_ws(pairs, attn4_units(pairs, (int64_t)max_tokens + nq_max), (int64_t)nq_max * (num_q_heads / num_kv_heads)).total;
+  const int64_t rows = (int64_t)nq_max * (num_q_heads / num_kv_heads);
+  return attn4_ws(pairs, attn4_units(pairs, (int64_t)max_tokens + nq_max, rows), rows).total;
 }
 
 dustin_status dustin_sparse_verify_attn_kv4(const void* q, int64_t q_sb, int64_t q_st, int64_t q_sh,

@@ -14,13 +14,16 @@
 // so that a wave holds an eighth of the accumulator, and nothing is left to add up at the end but the row sums.
 //
 // What it does not reach is memory's rate: a token is 136 bytes and, for each 16 query rows, 16 K multiply-adds, so
-// decoding, the value tile's way through LDS and the barrier of a round are in the way (vector unit 44 %, matrix unit
-// 27 %, LDS 40 % busy over a call).  Measured: 128 pairs of 2053 selected tokens and 40 rows 27.9 us and 4.7 for the
-// join (1.2 TB/s); the whole cache of 16 sequences of 4000 to 65536 tokens, 72 rows, pages of 16: 291 us (2.1 TB/s);
-// 16 pairs of 8192 tokens and 7 rows 11.6 and 3.9.  Other forms: two workgroups to a CU (one value tile, the queries
-// read from LDS, one round in flight) 26.7 for the first, 12.2 against 10.7 for the last; one value tile and two
-// barriers a round, 36 for the first with its join; every wave with tokens and an accumulator of its own, joined at the
-// end of a part, 46.
+// decoding, the value tile's way through LDS and the barriers of a round are in the way (with 40 rows: vector unit 44 %,
+// matrix unit 27 %, LDS 40 % busy over a call).  Up to 48 query rows the registers and LDS are cut down so that two
+// workgroups fit a CU, and where there is much to do (kAttn4Much) both are used: whole calls over 8 sequences of 32768
+// tokens and 8 KV heads take 70 us (8 rows, 4.1 TB/s), 91 (32) and 108 (40), with one workgroup to a CU, that has two
+// value tiles and more rounds in flight, 84, 107 and 119; the same over 4096 selected ones (2112 granules) 24, 27 and 31
+// either way with one workgroup to a CU, 24, 29 and 32 with two.  With more rows there is no room for a second:
+// 72 rows 133 us, 88 155, 128 221; 16 sequences of 4000 to 65536 tokens, 72 rows, pages of 16: 291 (2.1 TB/s).
+// Other forms: one value tile and two barriers a round with 72 rows 133, 88 161; the queries read from LDS as well
+// 148 and 176; every wave with tokens and an accumulator of its own, joined at the end of a part, 46 where this form at
+// its first took 36.
 #include "kv4.hpp"
 
 namespace dustin {
@@ -32,7 +35,6 @@ constexpr int kW4 = 8;                   // waves of a workgroup: two to a SIMD
 constexpr int kThreads4 = kW4 * kWave;
 constexpr float kRescale4 = 8.f;         // the references move when a row's maximum passes its own by 2^8
 constexpr float kNoRef = -3e38f;         // reference of a row that has seen no token: any score passes it
-constexpr int kRing4 = 8;                // rounds whose positions and pages a wave holds
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef short v4i16 __attribute__((ext_vector_type(4)));
@@ -141,21 +143,25 @@ __device__ __forceinline__ Pair4 pair_of(const Attn4Args& a, int pair) {
 }
 
 __device__ __forceinline__ int run_length(const Attn4Args& a, int total) {
-  return max(1, (int)(((int64_t)total + a.units - 1) / a.units));
+  const int units = total < kAttn4Much ? min(a.units, kAttn4Cus) : a.units;
+  return max(1, (int)(((int64_t)total + units - 1) / units));
 }
 
 template <int RT, bool kSparse, bool kPaged>
-__global__ __launch_bounds__(kThreads4) void attn_kv4_kernel(Attn4Args a) {
+__global__ __launch_bounds__(kThreads4, RT <= kAttn4Two ? 4 : 2) void attn_kv4_kernel(Attn4Args a) {
+  constexpr bool kTwo = RT <= kAttn4Two;         // two workgroups to a CU
   constexpr int kTpw = 16;                       // tokens of a wave's round
   constexpr int kTok = kW4 * kTpw;               // of a round
   constexpr int kRaw = kTpw * 136;               // a wave's rows and scales of a round as they come from memory
   constexpr int kRawLoads = 3;
-  constexpr int kSlots = RT <= 4 ? 3 : 2;        // rounds in flight
+  constexpr int kSlots = kTwo ? 1 : RT <= 4 ? 3 : 2;  // rounds in flight
+  constexpr int kAhead = kSlots == 1 ? 1 : 2;    // rounds from a position's load to its page's, and on to the rows'
+  constexpr int kRing4 = kSlots == 1 ? 4 : 8;    // rounds whose positions and pages a wave holds
   // Two V tiles and two sets of probabilities, so that a round's are written while others still read those of the round
-  // before: one barrier a round (where LDS holds them).
-  constexpr int kSets = RT <= 6 ? 2 : 1;
+  // before: one barrier a round (where LDS holds them).  Two workgroups hide each other's second barrier.
+  constexpr int kSets = !kTwo && RT <= 6 ? 2 : 1;
   constexpr int kExtra = (kSparse ? 1 : 0) + (kPaged ? 1 : 0);  // loads of positions and pages in a round
-  constexpr bool kQReg = RT <= 6;                // the queries in registers, else read from LDS in every round
+  constexpr bool kQReg = !kTwo && RT <= 6;       // the queries in registers, else read from LDS in every round
   constexpr int kQPitch = kD4 + 8;
   constexpr int kQBytes = RT * 16 * kQPitch * 2;
   constexpr int kVBytes = kTok * kD4 * 2;
@@ -296,7 +302,7 @@ __global__ __launch_bounds__(kThreads4) void attn_kv4_kernel(Attn4Args a) {
     const uint32_t pos_lane = lds_addr(pos_ring) + 4 * lr, page_lane = lds_addr(page_ring) + 4 * lr;
     if constexpr (kSparse) {
 #pragma unroll
-      for (int n = 0; n < kSlots + 4; ++n) load_pos(n);
+      for (int n = 0; n < kSlots + 2 * kAhead; ++n) load_pos(n);
     }
     // ---- queries, absent rows as zeros
     char* const sm_q = kQReg ? sm_v : sm_q_own;
@@ -313,7 +319,7 @@ __global__ __launch_bounds__(kThreads4) void attn_kv4_kernel(Attn4Args a) {
     if constexpr (kSparse) wait_loads<0>();
     if constexpr (kPaged) {
 #pragma unroll
-      for (int n = 0; n < kSlots + 2; ++n) load_page(n, kSparse ? read_word(pos_lane + ring_of(n)) : 0);
+      for (int n = 0; n < kSlots + kAhead; ++n) load_page(n, kSparse ? read_word(pos_lane + ring_of(n)) : 0);
       wait_loads<0>();
     }
 #pragma unroll
@@ -409,19 +415,19 @@ __global__ __launch_bounds__(kThreads4) void attn_kv4_kernel(Attn4Args a) {
       bf16x8 kop[4];
       if (next) {
         // this round's rows, and the positions and pages that the loads below read
-        wait_loads<(kSlots - 1) * kRawLoads + kExtra>();
+        wait_loads<kSlots == 1 ? 0 : (kSlots - 1) * kRawLoads + kExtra>();
         u32x4 kd, vd;
         uint32_t kse, vse;
         const uint32_t at_sel = pos_lane + ring_of(n + kSlots), at_page = page_lane + ring_of(n + kSlots);
-        const uint32_t at[3] = {kSparse ? at_sel : at_page, at_page, pos_lane + ring_of(n + kSlots + 2)};
+        const uint32_t at[3] = {kSparse ? at_sel : at_page, at_page, pos_lane + ring_of(n + kSlots + kAhead)};
         int word[3] = {0, 0, 0};
         read_raw<kSparse && kPaged ? 3 : kExtra>(raw_lane + slot_n * kRaw, raw_scale + slot_n * kRaw, at, kd, vd, kse, vse,
                                                  word);
 #pragma unroll
         for (int w = 0; w < 4; ++w)
           *reinterpret_cast<u32x4*>(v_at(set, wave * kTpw + lr, 4 * lg + w)) = kv4_decode8(vd[w], kv4_scale(vse));
-        load_pos(n + kSlots + 4);
-        load_page(n + kSlots + 2, word[2]);
+        load_pos(n + kSlots + 2 * kAhead);
+        load_page(n + kSlots + kAhead, word[2]);
         load_rows(n + kSlots, slot_n, kSparse ? word[0] : 0, kSparse ? word[1] : word[0]);
         slot_n = slot_n + 1 == kSlots ? 0 : slot_n + 1;
 #pragma unroll

@@ -98,6 +98,9 @@ hipError_t launch_evict(const EvictArgs& a, hipStream_t stream);
 
 // ---- verification attention over a 4-bit cache (attn_kv4.hip) ----
 constexpr int kAttn4Granule = 128;  // tokens
+constexpr int kAttn4Cus = 256;
+constexpr int kAttn4Two = 3;        // tiles of 16 query rows up to which two workgroups share a CU
+constexpr int kAttn4Much = 4096;    // granules from which on both are used
 
 struct Attn4Args {
   const uint16_t* q;

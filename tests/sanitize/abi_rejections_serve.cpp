@@ -234,6 +234,7 @@ int main() {
            BAD);
     EXPECT(dense(&k, &v, &bt, 8, nullptr), DUSTIN_ERR_WORKSPACE);
     EXPECT(dense(&k, &v, &bt, 8, fake(), (size_t)1 << 40, -1.f), BAD);
+    dustin_kv4 big_rows = kv4();
     const dustin_kv4 k64 = kv4(200, 2, 64);
     EXPECT(dense(&k64, &k64, &bt), UNSUP);
     dustin_batch b2 = batch(2, 100, 33);  // 33 x 4 rows of a head
@@ -241,13 +242,17 @@ int main() {
     b2 = batch(2, 100, 32);
     EXPECT(dense(&k, &v, &b2), PASSED);
     EXPECT(dustin::last_rt, 8);
+    b2 = batch(1, INT32_MAX - 4096, 32);
+    big_rows.capacity = INT32_MAX;
+    EXPECT(dense(&big_rows, &big_rows, &b2), PASSED);
+    EXPECT(dustin::last_units, 256);
     b2 = batch(40000, 100, 4);  // 80000 pairs
     EXPECT(dense(&k, &v, &b2), UNSUP);
     dustin_kv4 big = kv4();
     big.capacity = INT32_MAX;
     b2 = batch(1, INT32_MAX - 4096, 4);
     EXPECT(dense(&big, &big, &b2), PASSED);
-    EXPECT(dustin::last_units, 256);
+    EXPECT(dustin::last_units, 512);  // two workgroups to a CU
     b2 = batch(1, INT32_MAX - 4095, 4);
     EXPECT(dense(&big, &big, &b2), UNSUP);
     b2 = batch(2, 100, 4, INT32_MAX - 4095);

@@ -261,3 +261,31 @@ def test_row_past_four_gib():
     rows = U.rounded(x[0, :, 0].double().cpu().numpy())
     ref, tol = U.attention(q[0, 0].double().cpu().numpy(), rows, -rows, [300] * 8, 128 ** -0.5)
     assert (np.abs(out[0, 0].double().cpu().numpy() - ref) <= tol).all()
+
+
+@pytest.mark.parametrize("T,gs,paged", [(2, 4, False), (4, 8, True), (5, 8, False)])
+def test_batches_that_fill_the_chip_twice(T, gs, paged):
+    """Enough tokens (over 4096 granules of 128) for two workgroups on every CU, one, two and three tiles of query rows;
+    a sequence that ends inside a granule and one of a single token between long ones."""
+    H, lens, page = 8, [40000, 1, 27011], 64
+    cap = 40000 + 64
+    g = torch.Generator(device="cuda").manual_seed(T)
+    per = cap // page + 1
+    k, v = D.kv4_empty(3 * per if paged else 3, page if paged else cap, H, 128, "cuda")
+    table = torch.randperm(3 * per, generator=g, device="cuda").int().view(3, per) if paged else None
+    x = torch.randn(3, 5008, H, 128, generator=g, device="cuda").bfloat16()
+    y = torch.randn(3, 5008, H, 128, generator=g, device="cuda").bfloat16()
+    kw = dict(page_table=table)
+    for i in range(8):
+        D.kv4_append(x.roll(17 * i, 1), y.roll(5 * i, 1), k, v, [5008 * i] * 3, max_len=5008 * 7, **kw)
+    q = torch.randn(3, T, H * gs, 128, generator=g, device="cuda").bfloat16()
+    out = D.dense_verify_attn_kv4(q, k, v, lens, max_len=40000, **kw)
+    kk, vv = D.kv4_read(k, v, [0] * 3, n_query=[n + T for n in lens], nq_max=40000 + T, max_len=0, **kw)
+    torch.cuda.synchronize()
+    for b, n in enumerate(lens):
+        for h in (0, 3, 7):
+            rows = q[b, :, h * gs:(h + 1) * gs].double().cpu().numpy().reshape(-1, 128)
+            ref, tol = U.attention(rows, kk[b, :n + T, h].double().cpu().numpy(), vv[b, :n + T, h].double().cpu().numpy(),
+                                   np.repeat(n + 1 + np.arange(T), gs), 128 ** -0.5)
+            got = out[b, :, h * gs:(h + 1) * gs].double().cpu().numpy().reshape(-1, 128)
+            assert (np.abs(got - ref) <= tol).all(), f"sequence {b} head {h}"

@@ -194,12 +194,11 @@ def _i32(x, dev):
     return torch.tensor(list(x), dtype=torch.int32, device=dev)
 
 
-def _pages(need, cap, g, dev):
-    """A page table of `cap` positions whose rows are consecutive runs of a permutation of the pool, and the pool's
-    size."""
+def _pages(need, g, dev):
+    """A page table whose rows are consecutive runs of a permutation of the pool, and the pool's size."""
     per = [max(1, -(-x // PAGE)) for x in need]
     perm = torch.randperm(sum(per), generator=g, device=dev).to(torch.int32)
-    pt = torch.zeros((len(per), -(-cap // PAGE)), dtype=torch.int32, device=dev)
+    pt = torch.zeros((len(per), max(per)), dtype=torch.int32, device=dev)
     at = 0
     for b, p in enumerate(per):
         pt[b, :p] = perm[at:at + p]
@@ -308,8 +307,8 @@ def prepare(case, seed):
     n, t, k = _sizes(c)
     h, tmax, four = HKV[c["Hq"]], max(t), kind != "evict" or c["four"]
     need = [x + y for x, y in zip(n, t)]
-    cap = max(1, max(n) + tmax)  # what the calls of the batch may address
-    pt, pool = _pages(need, cap, g, dev) if c["paged"] else (None, 0)
+    pt, pool = _pages(need, g, dev) if c["paged"] else (None, 0)
+    cap = max(1, max(need))
     st.update(n=n, t=t, k=k, h=h, pt=pt, seq=_i32(n, dev), nq=_i32(t, dev), max_len=max(n))
     if four:
         st["kv"] = _cache4(n, cap, h, pt, pool, dev)
@@ -323,7 +322,7 @@ def prepare(case, seed):
     elif kind == "evict":
         st["idx"], st["cnt"] = _selection(n, k, g, dev)
         kmax = st["idx"].shape[2]
-        st["opt"], opool = _pages(k, kmax, g, dev) if c["paged"] else (None, 0)
+        st["opt"], opool = _pages(k, g, dev) if c["paged"] else (None, 0)
         st["wts"] = torch.rand((c["B"], 1, max(n)), generator=g, device=dev).square()
         st["wout"] = torch.zeros((c["B"], 1, kmax), device=dev)
         st["lens"] = torch.zeros(c["B"], dtype=torch.int32, device=dev)

@@ -519,7 +519,8 @@ dustin_status dustin_kv_commit(int32_t* seq_lens, const int32_t* accepted, const
  * below -125); each channel over the scale is the nearest element, of two as near the one with an even code, and 6
  * beyond 6.  An infinity counts as the largest finite bf16 of its sign, a NaN as zero.
  *   k_new, v_new  bf16 [B, nq_max, Hkv, d] (d 64 or 128), strides in elements, as dustin_kv_append
- *   k, v          the caches; must address max_len + nq_max positions per sequence
+ *   k, v          the caches; must address max_len + nq_max positions per sequence, with n_query max_len: then a sequence
+ *                 needs room (pages) for its own N_b + T_b alone; rows past a cache's end are not written
  *   bt            seq_lens (N_b), n_query (T_b, NULL = nq_max), max_len, nq_max
  * --------------------------------------------------------------------------------- */
 dustin_status dustin_kv4_append(const void* k_new, int64_t k_sb, int64_t k_st, int64_t k_sh, const void* v_new,
@@ -528,7 +529,8 @@ dustin_status dustin_kv4_append(const void* k_new, int64_t k_sb, int64_t k_st, i
 
 /* ---------------------------------------------------------------------------------
  * dustin_kv4_read -- the values of positions [N_b, N_b + T_b) of 4-bit caches, as bf16 (exact):
- *   k_out[b, t, h, :] = K[b, N_b + t, h, :], v_out alike, for t < T_b; other rows of the outputs are not written.
+ *   k_out[b, t, h, :] = K[b, N_b + t, h, :], v_out alike, for t < T_b; other rows of the outputs are not written, nor
+ *   those of positions past a cache's end.
  * With N_b = 0 and T_b the context it reads whole caches, for the entry points that take a bf16 cache (the scores).
  * Arguments as dustin_kv4_append's, with outputs in place of k_new and v_new.
  * --------------------------------------------------------------------------------- */
@@ -540,6 +542,7 @@ dustin_status dustin_kv4_read(void* k_out, int64_t k_sb, int64_t k_st, int64_t k
  * dustin_sparse_verify_attn_kv4, dustin_dense_verify_attn_kv4 -- dustin_sparse_verify_attn and dense_verify_attn over
  * 4-bit caches of 128 channels: the same sums, with K and V the values that the caches stand for.  Arguments, limits
  * and rounding are theirs, but for
+ *   - with n_query, the caches must address max_len positions alone (as dustin_kv4_append);
  *   - the caches' rows may lie anywhere a 64-bit offset reaches, pages need not be packed; strides of positions and of
  *     pages (data's and the scales') are below 2^32 bytes, and max_len and k_max at most 2^31 - 4097;
  *   - workspace: dustin_attn_kv4_workspace(...) bytes, 256-byte aligned, of any content.  Calls that share a

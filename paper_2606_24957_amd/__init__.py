@@ -961,6 +961,12 @@ def _kv4_pair(k: KV4, v: KV4, page_table) -> Tuple[DustinKV4, DustinKV4]:
     return kv4_view(k, page_table), kv4_view(v, page_table)
 
 
+def _kv4_max_len(kv, vv, nq_max, n_query) -> int:
+    """The longest sequence that the caches hold: beside nq_max window tokens, or, where each sequence has a number of
+    its own, beside none."""
+    return min(_capacity(kv), _capacity(vv)) - (nq_max if n_query is None else 0)
+
+
 def _kv4_rows(fn, what, k_rows, v_rows, k, v, seq_lens, n_query, page_table, max_len, stream, result) -> Call:
     _on_device(k_rows, v_rows)
     kv, vv = _kv4_pair(k, v, page_table)
@@ -973,7 +979,7 @@ def _kv4_rows(fn, what, k_rows, v_rows, k, v, seq_lens, n_query, page_table, max
     _holds(B, k.data, page_table)
     _holds(B, v.data, page_table)
     dev = k_rows.device
-    max_len = _capacity(kv) - nq_max if max_len is None else int(max_len)
+    max_len = _kv4_max_len(kv, vv, nq_max, n_query) if max_len is None else int(max_len)
     seq, nqa = _per_seq(seq_lens, B, dev, "seq_lens"), _per_seq(n_query, B, dev, "n_query")
     bt = _batch(B, max_len, nq_max, 0, seq, nqa)
     args = (_ptr(k_rows), k_rows.stride(0), k_rows.stride(1), k_rows.stride(2), _ptr(v_rows), v_rows.stride(0),
@@ -985,7 +991,7 @@ def _kv4_rows(fn, what, k_rows, v_rows, k, v, seq_lens, n_query, page_table, max
 def plan_kv4_append(k_new: torch.Tensor, v_new: torch.Tensor, k: KV4, v: KV4, seq_lens, *, n_query=None,
                     page_table: Optional[torch.Tensor] = None, max_len: Optional[int] = None, stream=None) -> Call:
     """Prepared dustin_kv4_append: k_new / v_new bf16 [B, T_max, Hkv, d] go, rounded into 4 bits, to positions
-    [N_b, N_b + T_b) of the caches."""
+    [N_b, N_b + T_b) of the caches, which with n_query need hold each sequence's own N_b + T_b alone."""
     return _kv4_rows(lib().dustin_kv4_append, "dustin_kv4_append", k_new, v_new, k, v, seq_lens, n_query, page_table,
                      max_len, stream, None)
 
@@ -1034,7 +1040,7 @@ def _plan_attn_kv4(q, k, v, idx, count, seq_lens, n_query, page_table, scale, ou
     if out.dtype != torch.bfloat16 or out.shape != q.shape or out.stride(3) != 1:
         raise ValueError("out must be bf16 of q's shape with contiguous rows")
     dev = q.device
-    max_len = _capacity(kv) - nq_max if max_len is None else int(max_len)
+    max_len = _kv4_max_len(kv, vv, nq_max, n_query) if max_len is None else int(max_len)
     seq, nqa = _per_seq(seq_lens, B, dev, "seq_lens"), _per_seq(n_query, B, dev, "n_query")
     scale = 1.0 / math.sqrt(d) if scale is None else scale
     k_max = 0 if idx is None else idx.shape[2]

@@ -57,6 +57,11 @@ dustin_status kv4_of(const dustin_kv4* kv, int64_t need, Kv4View* out) {
   return DUSTIN_OK;
 }
 
+// Positions that the caches of a batch must address.  Where every sequence has nq_max tokens: the longest one's and
+// theirs.  Where each has a count of its own, the longest may have the shortest window, which only the device knows:
+// max_len (an append writes nothing past a cache, and the attention's positions are clamped into it).
+int64_t positions_of(const dustin_batch* bt) { return (int64_t)bt->max_len + (bt->n_query ? 0 : bt->nq_max); }
+
 // K and V of one call: the same heads, channels and pages.
 template <class Kv>
 bool same_layout(const Kv* k, const Kv* v) {
@@ -75,7 +80,7 @@ dustin_status kv4_rows(bool append, const void* k_rows, int64_t k_sb, int64_t k_
   if (!same_layout(k, v)) return DUSTIN_ERR_INVALID_ARG;
   Kv4RowsArgs a;
   memset(&a, 0, sizeof a);
-  const int64_t need = (int64_t)bt->max_len + bt->nq_max;
+  const int64_t need = positions_of(bt);
   dustin_status st = kv4_of(k, need, &a.k);
   if (st == DUSTIN_OK) st = kv4_of(v, need, &a.v);
   if (st != DUSTIN_OK) return st;
@@ -150,7 +155,7 @@ dustin_status attn4(bool sparse, const void* q, int64_t q_sb, int64_t q_st, int6
   }
   Attn4Args a;
   memset(&a, 0, sizeof a);
-  const int64_t need = (int64_t)bt->max_len + bt->nq_max;
+  const int64_t need = positions_of(bt);
   dustin_status st = kv4_of(k, need, &a.k);
   if (st == DUSTIN_OK) st = kv4_of(v, need, &a.v);
   if (st != DUSTIN_OK) return st;

@@ -1,0 +1,106 @@
+// What the 4-bit cache and eviction entry points hand to their kernels, under AddressSanitizer and
+// UndefinedBehaviorSanitizer: built host-only together with csrc/api_kv4.hip, with the kernel launchers replaced by
+// stubs that keep the arguments and return an error (so that no call touches a device).  The bounds by which the kernels
+// clamp device values have to lie inside every cache of the call.  Prints one line per failed expectation and exits
+// non-zero if any failed.
+#include <stdio.h>
+#include <string.h>
+
+#include "../../paper_2606_24957_amd/csrc/kv4.hpp"
+
+namespace dustin {
+static Kv4RowsArgs rows_args;
+static Attn4Args attn_args;
+static EvictArgs evict_args;
+hipError_t launch_kv4_append(const Kv4RowsArgs& a, hipStream_t) { return rows_args = a, hipErrorInvalidValue; }
+hipError_t launch_kv4_read(const Kv4RowsArgs& a, hipStream_t) { return rows_args = a, hipErrorInvalidValue; }
+hipError_t launch_evict(const EvictArgs& a, hipStream_t) { return evict_args = a, hipErrorInvalidValue; }
+hipError_t launch_attn_kv4(const Attn4Args& a, int, bool, bool, hipStream_t) { return attn_args = a, hipErrorInvalidValue; }
+}  // namespace dustin
+
+static int failures = 0;
+#define EXPECT(call, want)                                                                              \
+  do {                                                                                                  \
+    const long long got_ = (long long)(call), want_ = (long long)(want);                                \
+    if (got_ != want_) {                                                                                \
+      printf("FAIL line %d: %s -> %lld, expected %lld\n", __LINE__, #call, got_, want_);                \
+      ++failures;                                                                                       \
+    }                                                                                                   \
+  } while (0)
+#define BAD DUSTIN_ERR_INVALID_ARG
+#define PASSED DUSTIN_ERR_LAUNCH  // validation let the call through to the (stubbed) launch
+
+static char* fake(size_t off = 0) { return reinterpret_cast<char*>(0x10000) + off; }
+template <class T>
+static T* at(size_t off = 0) {
+  return reinterpret_cast<T*>(fake(off));
+}
+static dustin_batch batch(int B, int max_len, int nq, bool own_counts, int k_max = 40) {
+  dustin_batch bt;
+  memset(&bt, 0, sizeof bt);
+  bt.batch = B;
+  bt.max_len = max_len;
+  bt.nq_max = nq;
+  bt.k_max = k_max;
+  bt.seq_lens = at<int32_t>();
+  bt.n_query = own_counts ? at<int32_t>() : nullptr;
+  return bt;
+}
+static dustin_kv4 kv4(int64_t n, size_t off = 0, int H = 2) {
+  dustin_kv4 c;
+  memset(&c, 0, sizeof c);
+  c.data = fake(off);
+  c.scales = fake(off);
+  c.num_kv_heads = H;
+  c.head_dim = 128;
+  c.stride_h = 64;
+  c.stride_n = H * c.stride_h;
+  c.stride_b = n * c.stride_n;
+  c.scale_stride_h = 4;
+  c.scale_stride_n = H * c.scale_stride_h;
+  c.scale_stride_b = n * c.scale_stride_n;
+  c.capacity = n;
+  return c;
+}
+static dustin_kv4 paged4(int pages, size_t off = 0) {
+  dustin_kv4 c = kv4(16, off);
+  c.page_table = at<int32_t>();
+  c.page_size = 16;
+  c.max_pages = pages;
+  c.num_pages = 30;
+  c.stride_page = 16 * c.stride_n;
+  c.scale_stride_page = 16 * c.scale_stride_n;
+  return c;
+}
+static int rows(bool append, const dustin_kv4& k, const dustin_kv4& v, const dustin_batch& bt) {
+  return append ? dustin_kv4_append(fake(), 2304, 256, 128, fake(), 2304, 256, 128, &k, &v, &bt, nullptr)
+                : dustin_kv4_read(fake(), 2304, 256, 128, fake(), 2304, 256, 128, &k, &v, &bt, nullptr);
+}
+static int attn(bool sparse, const dustin_kv4& k, const dustin_kv4& v, const dustin_batch& bt, int Hq = 8,
+                size_t bytes = (size_t)1 << 40) {
+  return sparse ? dustin_sparse_verify_attn_kv4(fake(), 9216, 1024, 128, Hq, &k, &v, &bt, at<int32_t>(), 40, 40,
+                                                at<int32_t>(), 1, 0.1f, fake(), 9216, 1024, 128, fake(), bytes, nullptr)
+                : dustin_dense_verify_attn_kv4(fake(), 9216, 1024, 128, Hq, &k, &v, &bt, 0.1f, fake(), 9216, 1024, 128,
+                                               fake(), bytes, nullptr);
+}
+
+int main() {
+  // ---- sequences with window lengths of their own: the longest sequence may have the shortest window
+  for (const bool four_pages : {false, true}) {
+    const dustin_kv4 k = four_pages ? paged4(4) : kv4(64), v = four_pages ? paged4(4, 1 << 20) : kv4(64, 1 << 20);
+    for (const bool second : {false, true}) {
+      EXPECT(rows(second, k, v, batch(2, 63, 9, true)), PASSED);
+      EXPECT(rows(second, k, v, batch(2, 64, 9, true)), PASSED);
+      EXPECT(rows(second, k, v, batch(2, 65, 9, true)), BAD);
+      EXPECT(rows(second, k, v, batch(2, 55, 9, false)), PASSED);
+      EXPECT(rows(second, k, v, batch(2, 56, 9, false)), BAD);
+      EXPECT(attn(second, k, v, batch(2, 63, 9, true)), PASSED);
+      EXPECT(attn(second, k, v, batch(2, 64, 9, true)), PASSED);
+      EXPECT(attn(second, k, v, batch(2, 65, 9, true)), BAD);
+      EXPECT(attn(second, k, v, batch(2, 55, 9, false)), PASSED);
+      EXPECT(attn(second, k, v, batch(2, 56, 9, false)), BAD);
+    }
+  }
+  printf("%s: %d failed expectations\n", failures ? "FAILED" : "ok", failures);
+  return failures ? 1 : 0;
+}

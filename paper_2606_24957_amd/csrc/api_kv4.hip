@@ -159,6 +159,7 @@ dustin_status attn4(bool sparse, const void* q, int64_t q_sb, int64_t q_st, int6
   dustin_status st = kv4_of(k, need, &a.k);
   if (st == DUSTIN_OK) st = kv4_of(v, need, &a.v);
   if (st != DUSTIN_OK) return st;
+  a.k.capacity = a.v.capacity = a.k.capacity < a.v.capacity ? a.k.capacity : a.v.capacity;  // a token is a row of both
   // the kernels multiply positions and pages by 32-bit strides, and count granules in 32 bits
   for (const Kv4View* c : {&a.k, &a.v})
     for (const int64_t x : {c->stride_n, c->sstride_n, c->stride_page, c->sstride_page})

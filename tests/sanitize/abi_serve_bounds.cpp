@@ -101,6 +101,13 @@ int main() {
       EXPECT(attn(second, k, v, batch(2, 56, 9, false)), BAD);
     }
   }
+  // ---- K and V of different capacity: a selected position is clamped into both
+  for (const bool v_is_shorter : {false, true}) {
+    const dustin_kv4 a = kv4(200), b = kv4(104, 1 << 20);
+    EXPECT(attn(true, v_is_shorter ? a : b, v_is_shorter ? b : a, batch(2, 100, 4, false)), PASSED);
+    EXPECT(dustin::attn_args.k.capacity, 104);
+    EXPECT(dustin::attn_args.v.capacity, 104);
+  }
   printf("%s: %d failed expectations\n", failures ? "FAILED" : "ok", failures);
   return failures ? 1 : 0;
 }

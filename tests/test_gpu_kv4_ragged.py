@@ -56,3 +56,19 @@ def test_no_room_but_each_ones_own(seq, nq, stated, ps):
             np.testing.assert_array_equal(got[b, :nq[b]].double().cpu().numpy(), held[where][seq[b]:])
     check(dense, q, k, v, pt, ps, seq, nq, lambda b, h: np.arange(seq[b]), 128 ** -0.5)
     check(sparse, q, k, v, pt, ps, seq, nq, lambda b, h: sel[b], 128 ** -0.5)
+
+
+@pytest.mark.parametrize("long_k", [False, True])
+def test_positions_outside_the_shorter_cache(long_k):
+    """K and V of different lengths: a selected position past the shorter one counts as its last."""
+    n, more, H = 60, 4000, 2
+    x = torch.randn((2, 1, n + 1, H, 128), device=DEV, dtype=torch.bfloat16)
+    k, v = (D.kv4_empty(1, n + 1 + (more if long_k == (i == 0) else 0), H, 128, DEV)[i] for i in range(2))
+    k, v = (D.KV4(c.data.clone(), c.scales.clone()) for c in (k, v))
+    D.kv4_append(x[0], x[1], k, v, [0], max_len=0)
+    q = torch.randn((1, 1, 4 * H, 128), device=DEV, dtype=torch.bfloat16)
+    idx = i32([3, 59, 60, 61, 4000, 2 ** 31 - 1, -5]).view(1, 1, -1)
+    out = torch.full_like(q, float("nan"))
+    D.sparse_verify_attn_kv4(q, k, v, idx, i32([7]).view(1, 1), i32([n]), out=out)
+    torch.cuda.synchronize()
+    check(out, q, k, v, None, 0, [n], [1], lambda b, h: [3, 59, 60, 60, 60, 60, 0], 128 ** -0.5)

@@ -320,14 +320,14 @@ __device__ __forceinline__ uint64_t block_before(uint64_t x, uint64_t* sm, uint6
   return at_lane(sums - own, wave) + incl - x;
 }
 
-// What a chunk's sums of weights are multiplied by to be against the row's largest logit.
+// What a chunk's sums of weights are multiplied by to be against the row's largest logit: zero where not even its best
+// token has a weight in the row (its others, against that one, may have), so that a chunk with a sum holds such a token.
 __device__ __forceinline__ double rescaled(const Exp2& exp2, float c_top, float top, double scale) {
   if (c_top == top) return 1.0;
-  const double d = ((double)c_top - (double)top) * scale;
-  return d > -46.0 ? exp2(d) : d > -110.0 ? exp2(d + 64.0, -64) : 0.0;
+  return units_of(exp2, c_top, top, scale) ? exp2(exponent_of(c_top, top, scale)) : 0.0;
 }
 __device__ __forceinline__ uint64_t scaled(uint64_t sum, double factor) {
-  return factor == 1.0 ? sum : (uint64_t)((double)sum * factor);
+  return factor == 1.0 ? sum : (uint64_t)__builtin_rint((double)sum * factor);
 }
 
 // Both at once: the sums before this thread, and in all.

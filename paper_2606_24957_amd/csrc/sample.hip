@@ -24,6 +24,7 @@ constexpr int kRowWaves = kRowThreads / kWave;
 static_assert(kSamplePieces == kRowThreads, "a piece to a thread");
 constexpr int kFew = kSampleFew, kList = kSampleList;
 constexpr int kPairs = 128;  // tokens that are compared each with each
+constexpr int kCutBin = 8 * (kSampleFrac + 1) - 1;  // first eighth that a weight below half a unit can fall in
 
 // 2^(d + up) for -46 <= d <= 46, to within 2^-47: 2^d = 2^n 2^f, |f| <= 1/2, and the Taylor series of e^(f ln 2) to the
 // 11th power (the next term is below 2^-47).  The coefficients are held in scalar registers (as literals, each would be
@@ -654,6 +655,11 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
     plan.mode = sm_u64[0] + in <= kFew ? kRowFew : in <= kList && !p_of_k && !s.counts_do() ? kRowList : kRowRead;
     plan.bin = bin;
     plan.hi = whole_key(bin_key(top, s.scale, bin));
+    // From here on an eighth can hold tokens without a weight, which the chunks count against their own largest logits
+    // or not at all.  The list leaves them out, so that it never has more than what was counted.
+    if (bin >= kCutBin)
+      plan.hi = min(plan.hi, whole_key(least_key(top, (double)top - 45.0 / s.scale,
+                                                 [&](float x) { return units_of(exp2, x, top, s.scale) != 0; })));
     plan.lo = plan.mode == kRowList && bin > 0 ? whole_key(bin_key(top, s.scale, bin - 1)) + 1 : 0;
     plan.before_cnt = plan.mode == kRowList ? sm_u64[0] : 0;
     plan.before_sum = plan.mode == kRowList ? sm_u64[1] : 0;

@@ -64,3 +64,40 @@ def test_the_only_token_of_a_chunk_just_above_the_cut(dtype):
     token = D.sample(x, u)
     torch.cuda.synchronize()
     assert token.tolist() == [7, 16000]
+
+
+def peaks(V, n, top, rest, place):
+    """Every chunk of n tokens has one high logit (at its first, middle or last place), all others are `rest`."""
+    x = torch.full((V,), float(rest))
+    for c in range(0, V, n):
+        size = min(n, V - c)
+        x[c + {"first": 0, "middle": size // 2, "last": size - 1}[place]] = top - 0.0625 * (c // n)
+    return x
+
+
+@pytest.mark.parametrize("place", ["first", "middle", "last"])
+@pytest.mark.parametrize("dtype,n", [(torch.float32, 4096), (torch.bfloat16, 8192)])
+@pytest.mark.parametrize("V", [8190, 32000, 151936])
+@pytest.mark.parametrize("top,rest,settings", [
+    (0.0, -31.5, (1.0, 1000, 1.0, 0.0)),       # a top_k that the tokens with a weight do not reach
+    (0.0, -31.5, (1.0, 3000, 0.999, 0.0)),
+    (0.0, -31.5, (1.0, 1000, 1.0, 0.01)),
+    (0.078125, -31.15, (1.0, 0, 1.0, 2.85e-14)),  # min_p ends in the eighth of an octave that the cut runs through
+    (0.0, -31.75, (1.0, 512, 1.0, 0.0)),       # counts alone decide
+    (0.0, -31.75, (1.0, 300, 0.9, 0.0)),
+])
+def test_lists_leave_out_what_has_no_weight(top, rest, settings, V, dtype, n, place):
+    """Thousands of tokens just below the cut compete with none of those that have a weight for a place in a list."""
+    x = peaks(V, n, top, rest, place)
+    if V > 3 * n and settings[1] in (300, 512):  # a chunk whose best lies lower: its tokens below the cut are counted
+        x[2 * n:3 * n] = float("-inf")
+        x[2 * n:2 * n + 100] = rest
+        x[2 * n + 50] = -0.25
+    x = x.to(dtype).to(DEV).expand(4, V).contiguous()
+    u = torch.tensor([0.0, 0.3, 0.7, 1.0 - 2.0 ** -24], device=DEV)
+    probs = torch.full((4, V), float("nan"), device=DEV)
+    kw = dict(temperature=settings[0], top_k=settings[1], top_p=settings[2], min_p=settings[3])
+    token, _ = D.sample(x, u, probs=probs, **kw)
+    torch.cuda.synchronize()
+    for b in range(4):
+        check(x[b], token[b], float(u[b]), probs[b], settings)

@@ -583,7 +583,8 @@ dustin_status dustin_dense_verify_attn_kv4(const void* q, int64_t q_sb, int64_t 
  *       the cache counts as its nearest end; groups 1 or the KV head count
  *   w, w_out    fp32 [B, groups, >= w_len], [B, groups, >= k_max] (strides in elements) or both NULL; w_out may be w
  *   new_lens    int32 [B] or NULL; may be the batch's seq_lens, which this call does not read
- * A step's layers share idx: pass w and new_lens with one of them.
+ * A step's layers share idx: pass w and new_lens with one of them.  Without any cache (k, v, k_out and v_out NULL) the
+ * weights alone are moved, for any number of groups: other arrays over the same positions, such as a history.
  * --------------------------------------------------------------------------------- */
 dustin_status dustin_kv_evict(const dustin_kv* k, const dustin_kv* v, const dustin_kv* k_out, const dustin_kv* v_out,
                               int32_t batch, const int32_t* idx, int64_t idx_sb, int64_t idx_sg, const int32_t* count,

@@ -1104,16 +1104,19 @@ def plan_kv_evict(k, v, idx: torch.Tensor, count: torch.Tensor, *, k_out=None, v
                   new_lens: Optional[torch.Tensor] = None, stream=None) -> Call:
     """Prepared dustin_kv_evict (bf16 caches) or dustin_kv4_evict (KV4): a layer's rows idx[b, g, :count] to the front
     of k_out / v_out (with out_page_table), or of the caches themselves where no outputs are given.  v None: k alone
-    (a cache of keys that the scores read).  weights fp32 [B, G, N] go the same way into weights_out (None: in place),
-    new_lens int32 [B] becomes the counts.  A page that two sequences share must not be written."""
+    (a cache of keys that the scores read); k and v None: the weights alone.  weights fp32 [B, G, N] go the same way
+    into weights_out (None: in place), new_lens int32 [B] becomes the counts.  A page that two sequences share must not
+    be written."""
     four = isinstance(k, KV4)
+    if k is None and (weights is None or any(x is not None for x in (v, k_out, v_out, page_table, out_page_table))):
+        raise ValueError("without k, only weights can be moved")
     if any(isinstance(x, KV4) != four for x in (v, k_out, v_out) if x is not None):
         raise ValueError("k, v, k_out and v_out are bf16 caches or KV4 caches")
     if (v is not None and (k_out is None) != (v_out is None)) or (v is None and v_out is not None):
         raise ValueError("outputs for each of the caches, or for none")
     if v is not None and (k.data if four else k).data_ptr() == (v.data if four else v).data_ptr():
         raise ValueError("k and v are one cache: give it as k alone")
-    if k_out is None:
+    if k_out is None and k is not None:
         if out_page_table is not None:
             raise ValueError("in place, the pages stay: out_page_table goes with outputs")
         k_out, v_out, out_page_table = k, v, page_table

@@ -241,13 +241,14 @@ dustin_status evict(const Kv* k, const Kv* v, const Kv* k_out, const Kv* v_out, 
                     int64_t idx_sb, int64_t idx_sg, const int32_t* count, int32_t groups, int32_t k_max, const float* w,
                     int64_t w_sb, int64_t w_sg, int32_t w_len, float* w_out, int64_t wo_sb, int64_t wo_sg,
                     int32_t* new_lens, int row_bytes_per_dim2, bool four, void* stream) {
-  if (!k || !k_out || !v != !v_out || batch < 0 || k_max < 0) return DUSTIN_ERR_INVALID_ARG;
+  const bool rows = k || v || k_out || v_out;  // else the weights alone
+  if ((rows ? !k || !k_out || !v != !v_out : !w) || batch < 0 || k_max < 0) return DUSTIN_ERR_INVALID_ARG;
   if (batch > 0 && ((!idx && k_max > 0) || !count)) return DUSTIN_ERR_INVALID_ARG;
-  if ((v && (!same_layout(k, v) || !same_layout(k_out, v_out))) || k->num_kv_heads != k_out->num_kv_heads ||
-      k->head_dim != k_out->head_dim)
+  if (rows && ((v && (!same_layout(k, v) || !same_layout(k_out, v_out))) || k->num_kv_heads != k_out->num_kv_heads ||
+               k->head_dim != k_out->head_dim))
     return DUSTIN_ERR_INVALID_ARG;
   if (v && (k->data == v->data || k_out->data == v_out->data)) return DUSTIN_ERR_INVALID_ARG;
-  if (groups != 1 && groups != k->num_kv_heads) return DUSTIN_ERR_INVALID_ARG;
+  if (rows ? groups != 1 && groups != k->num_kv_heads : groups < 1) return DUSTIN_ERR_INVALID_ARG;
   if (!aligned(idx, 4) || !aligned(count, 4) || !aligned(new_lens, 4) || idx_sb < 0 || idx_sg < 0)
     return DUSTIN_ERR_INVALID_ARG;
   if (!w != !w_out || !aligned(w, 4) || !aligned(w_out, 4)) return DUSTIN_ERR_INVALID_ARG;
@@ -255,15 +256,22 @@ dustin_status evict(const Kv* k, const Kv* v, const Kv* k_out, const Kv* v_out, 
   if (w && ((groups > 1 && wo_sg == 0) || (batch > 1 && wo_sb == 0))) return DUSTIN_ERR_INVALID_ARG;  // one row for several
   EvictArgs a;
   memset(&a, 0, sizeof a);
-  dustin_status st = evict_cache(k, 1, &a.src[0]);
-  if (st == DUSTIN_OK && v) st = evict_cache(v, 1, &a.src[1]);
-  if (st == DUSTIN_OK) st = evict_cache(k_out, k_max, &a.dst[0]);
-  if (st == DUSTIN_OK && v) st = evict_cache(v_out, k_max, &a.dst[1]);
-  if (st != DUSTIN_OK) return st;
-  const bool same_k = same_cache(a.src[0], a.dst[0], k->num_kv_heads, batch);
-  const bool same_v = v ? same_cache(a.src[1], a.dst[1], k->num_kv_heads, batch) : same_k;
-  if (same_k != same_v || (!same_k && (k->data == k_out->data || (v && v->data == v_out->data)))) return DUSTIN_ERR_INVALID_ARG;
-  a.caches = v ? 2 : 1;
+  if (rows) {
+    dustin_status st = evict_cache(k, 1, &a.src[0]);
+    if (st == DUSTIN_OK && v) st = evict_cache(v, 1, &a.src[1]);
+    if (st == DUSTIN_OK) st = evict_cache(k_out, k_max, &a.dst[0]);
+    if (st == DUSTIN_OK && v) st = evict_cache(v_out, k_max, &a.dst[1]);
+    if (st != DUSTIN_OK) return st;
+    const bool same_k = same_cache(a.src[0], a.dst[0], k->num_kv_heads, batch);
+    const bool same_v = v ? same_cache(a.src[1], a.dst[1], k->num_kv_heads, batch) : same_k;
+    if (same_k != same_v || (!same_k && (k->data == k_out->data || (v && v->data == v_out->data))))
+      return DUSTIN_ERR_INVALID_ARG;
+    a.caches = v ? 2 : 1;
+    a.num_kv_heads = k->num_kv_heads;
+    a.row_bytes = k->head_dim * row_bytes_per_dim2 / 2;
+    a.scale_bytes = four ? k->head_dim / kKv4Block : 0;
+    a.in_place = same_k;
+  }
   if (batch == 0) return DUSTIN_OK;
   a.idx = idx;
   a.idx_sb = idx_sb;
@@ -278,12 +286,8 @@ dustin_status evict(const Kv* k, const Kv* v, const Kv* k_out, const Kv* v_out, 
   a.new_lens = new_lens;
   a.batch = batch;
   a.groups = groups;
-  a.num_kv_heads = k->num_kv_heads;
   a.k_max = k_max;
   a.w_len = w_len;
-  a.row_bytes = k->head_dim * row_bytes_per_dim2 / 2;
-  a.scale_bytes = four ? k->head_dim / kKv4Block : 0;
-  a.in_place = same_k;
   return launch_evict(a, static_cast<hipStream_t>(stream)) == hipSuccess ? DUSTIN_OK : DUSTIN_ERR_LAUNCH;
 }
 

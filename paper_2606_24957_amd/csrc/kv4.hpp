@@ -81,7 +81,7 @@ struct EvictCache {
 };
 struct EvictArgs {
   EvictCache src[2], dst[2];  // K, V
-  int32_t caches;             // 2, or 1: K alone
+  int32_t caches;             // 2, or 1: K alone, or 0: the weights alone
   const int32_t* idx;
   int64_t idx_sb, idx_sg;
   const int32_t* count;

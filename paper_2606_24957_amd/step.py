@@ -153,11 +153,15 @@ class VerifyStep:
 
     def evict(self, weights: torch.Tensor, keep: int):
         """Cuts every cache, in place, to the keep positions of each sequence with the largest weights (fp32
-        [B, 1, >= n_max], such as the accumulated target scores s_t), sinks and recent ones among them; the weights and
-        the lengths follow.  Returns (idx, count)."""
+        [B, 1, >= n_max], such as the accumulated target scores s_t), sinks and recent ones among them; the weights, the
+        estimation's arrays over the positions (a history, given draft scores) and the lengths follow.  Behind the kept
+        positions these arrays are zero: positions to come have no history.  Returns (idx, count)."""
         s, first = self.s, self.layers[0]
         idx, cnt = topk(None, weights, self.seq, keep, n_sink=s.n_sink, n_window=s.n_window)
-        kv_evict(first.k, first.v, idx, cnt, page_table=first.page_table, weights=weights, new_lens=self.seq)
+        arrays = {x.data_ptr(): x for x in (weights, self.est.init_target, self.est.s_draft_given) if x is not None}
+        for x in arrays.values():
+            self._cut(x, idx, cnt)
+        kv_evict(first.k, first.v, idx, cnt, page_table=first.page_table, new_lens=self.seq)
         for L in self.layers[1:]:
             kv_evict(L.k, L.v, idx, cnt, page_table=L.page_table)
         if self.score_k is not first.k:
@@ -165,6 +169,17 @@ class VerifyStep:
         for k in self.est.draft_k:
             kv_evict(k, None, idx, cnt)
         return idx, cnt
+
+    @staticmethod
+    def _cut(x, idx, cnt):
+        """An array over the positions, fp32 [B, 1, N], follows the kept ones; zero behind them, and for positions past
+        its end (tokens that were accepted since it was written)."""
+        N = x.shape[2]
+        kept = idx[:, :, :N]
+        kv_evict(None, None, kept, cnt, weights=x)
+        stays = torch.arange(N, device=x.device) < cnt.unsqueeze(2)
+        stays[:, :, :kept.shape[2]] &= kept < N
+        x.masked_fill_(~stays, 0.0)
 
 
 def draft_layer_of(layer: int, n_target: int, n_draft: int) -> int:

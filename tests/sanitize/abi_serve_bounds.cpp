@@ -108,6 +108,25 @@ int main() {
     EXPECT(dustin::attn_args.k.capacity, 104);
     EXPECT(dustin::attn_args.v.capacity, 104);
   }
+  // ---- eviction of weights without a cache
+  {
+    auto alone = [&](const float* w, float* wo, int groups, int w_len, const int32_t* count) {
+      return (int)dustin_kv_evict(nullptr, nullptr, nullptr, nullptr, 2, at<int32_t>(), 40, 40, count, groups, 40, w, 200,
+                                  40, w_len, wo, 200, 40, nullptr, nullptr);
+    };
+    const dustin_kv4 k = kv4(200);
+    EXPECT(alone(at<float>(), at<float>(), 1, 200, at<int32_t>()), PASSED);
+    EXPECT(dustin::evict_args.caches, 0);
+    EXPECT(alone(at<float>(), at<float>(), 5, 200, at<int32_t>()), PASSED);
+    EXPECT(alone(at<float>(), at<float>(), 0, 200, at<int32_t>()), BAD);
+    EXPECT(alone(nullptr, nullptr, 1, 200, at<int32_t>()), BAD);
+    EXPECT(alone(at<float>(), nullptr, 1, 200, at<int32_t>()), BAD);
+    EXPECT(alone(at<float>(), at<float>(), 1, 0, at<int32_t>()), BAD);
+    EXPECT(alone(at<float>(), at<float>(), 1, 200, nullptr), BAD);
+    EXPECT(dustin_kv4_evict(nullptr, nullptr, &k, nullptr, 2, at<int32_t>(), 40, 40, at<int32_t>(), 1, 40, at<float>(),
+                            200, 40, 200, at<float>(), 200, 40, nullptr, nullptr),
+           BAD);
+  }
   printf("%s: %d failed expectations\n", failures ? "FAILED" : "ok", failures);
   return failures ? 1 : 0;
 }

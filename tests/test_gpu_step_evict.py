@@ -1,0 +1,116 @@
+"""The verification step after an eviction: what it scores and selects by is what a step planned anew over the cut caches
+and the cut arrays would."""
+import pytest
+import torch
+
+import paper_2606_24957_amd as D
+from paper_2606_24957_amd import step as S
+from paper_2606_24957_amd import workloads as W
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def build(name):
+    if name == "tiny":  # a history, and the draft scores given
+        s = W.config("tiny").replace(B=2, seq_lens=(2000, 700), n_query=(5, 3), budget=(256, 200), m=(118, 90))
+    elif name == "one":  # one sequence, one layer
+        s = W.config("tiny")
+    else:  # a history, three draft layers, two target layers
+        s = W.config("qwen7b").replace(B=2, seq_lens=(2000, 700), n_query=(5, 5), budget=(256, 256), m=(118, 118),
+                                       planted=(20,), layers=2)
+    layers = [W.make_layer(s, l, DEV) for l in range(s.layers)]
+    est = W.make_estimation(s, layers[0], DEV)
+    assert est.init_target is not None
+    return s, layers, est
+
+
+def cut(x, idx, cnt):
+    """Arrays over positions, cut by the definition: the kept entries in order, nothing behind them."""
+    y = torch.zeros_like(x)
+    for b in range(x.shape[0]):
+        at = idx[b, 0, :int(cnt[b, 0])].long()
+        inside = at < x.shape[2]
+        y[b, 0, :len(at)][inside] = x[b, 0, at[inside]]
+    return y
+
+
+def anew(s, st, est_arrays, est):
+    """A step planned over copies of what the evicted one holds, with the arrays given."""
+    layers = [W.Layer(l.q, l.k.clone(), l.v.clone(), l.page_table) for l in st.layers]
+    est2 = W.Estimation(est.q_target, est_arrays[0], est_arrays[1], est.draft_q, [k.clone() for k in est.draft_k])
+    st2 = S.VerifyStep(s, layers, est2, DEV, windows=st.windows)
+    st2.seq.copy_(st.seq)
+    return st2
+
+
+def same(s, a, b, lens):
+    assert torch.equal(a.cnt, b.cnt)
+    for i, n in enumerate(lens):
+        c = int(a.cnt[i, 0])
+        assert torch.equal(a.s_t[i, :, :n], b.s_t[i, :, :n]), f"sequence {i}: scores"
+        assert torch.equal(a.s_d[i, :, :n], b.s_d[i, :, :n]), f"sequence {i}: draft scores"
+        assert torch.equal(a.idx[i, 0, :c], b.idx[i, 0, :c]), f"sequence {i}: selection"
+        for x, y in zip(a.outs, b.outs):
+            assert torch.equal(x[i, :s.n_query[i]].view(torch.int16), y[i, :s.n_query[i]].view(torch.int16))
+
+
+@pytest.mark.parametrize("captured", [False, True])
+@pytest.mark.parametrize("by", ["scores", "history", "own"])
+@pytest.mark.parametrize("name", ["tiny", "one", "history"])
+def test_the_step_after_an_eviction(name, by, captured):
+    s, layers, est = build(name)
+    st = S.VerifyStep(s, layers, est, DEV)
+    st.run()
+    if captured:
+        st.capture()
+    torch.cuda.synchronize()
+    weights = {"scores": st.s_t, "history": est.init_target, "own": torch.rand((s.B, 1, s.n_max + 9), device=DEV)}[by]
+    old = [None if x is None else x.clone() for x in (est.init_target, est.s_draft_given, weights)]
+    idx, cnt = st.evict(weights, 150)
+    torch.cuda.synchronize()
+    lens = [min(150, n) for n in s.seq_lens]
+    assert st.seq.tolist() == lens
+    want = [None if x is None else cut(x, idx, cnt) for x in old]
+    for x, y in zip((est.init_target, est.s_draft_given, weights), want):
+        assert (x is None) == (y is None)
+        assert x is None or torch.equal(x, y)
+    st2 = anew(s, st, want[:2], est)
+    for _ in range(2):  # the next step, and the one after it with every token kept: new positions have no history
+        st.replay() if captured else st.run()
+        st2.run()
+        torch.cuda.synchronize()
+        same(s, st, st2, lens)
+        for x in (st, st2):
+            x.commit(x.nq)
+        torch.cuda.synchronize()
+        lens = [n + t for n, t in zip(lens, s.n_query)]
+        assert st.seq.tolist() == lens
+
+
+def test_weights_alone():
+    """Arrays over the positions without a cache, to others and in place, several groups."""
+    g = torch.Generator(device=DEV).manual_seed(1)
+    B, G, N, K = 3, 4, 5000, 4001
+    w = torch.rand((B, G, N), generator=g, device=DEV)
+    idx = torch.sort(torch.rand((B, G, N), generator=g, device=DEV).argsort(-1)[:, :, :K]).values.int()
+    cnt = torch.randint(0, K + 1, (B, G), generator=g, device=DEV).int()
+    cnt[0, 0], cnt[1, 1] = 0, K
+    lens = torch.full((B,), -1, dtype=torch.int32, device=DEV)
+    out = torch.full((B, G, K), -1.0, device=DEV)
+    want, inplace = out.clone(), w.clone()
+    for b in range(B):
+        for j in range(G):
+            c = int(cnt[b, j])
+            want[b, j, :c] = w[b, j, idx[b, j, :c].long()]
+            inplace[b, j, :c] = want[b, j, :c]
+    D.kv_evict(None, None, idx, cnt, weights=w, weights_out=out, new_lens=lens)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and torch.equal(lens, cnt[:, 0])
+    assert D.kv_evict(None, None, idx, cnt, weights=w) == (None, None)
+    torch.cuda.synchronize()
+    assert torch.equal(w, inplace)
+    with pytest.raises(ValueError, match="only weights"):
+        D.kv_evict(None, None, idx, cnt, new_lens=lens)
+    with pytest.raises(ValueError, match="only weights"):
+        D.kv_evict(None, None, idx, cnt, weights=w, k_out=out)

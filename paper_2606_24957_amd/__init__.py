@@ -445,6 +445,7 @@ def score_layers(qs, ks, seq_lens, heads, **kw):
 
 
 DIGIT_BINS = 4096
+TOPK_MAX_LEN = 1 << 19  # positions of a row that dustin_topk takes
 
 
 def digit_hist(rows: int, device) -> torch.Tensor:

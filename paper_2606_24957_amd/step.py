@@ -14,9 +14,9 @@ from typing import List, Optional
 
 import torch
 
-from . import (KV4, digit_hist, kv4_append, kv4_empty, kv_evict, plan_kv4_append, plan_kv_append, plan_kv_commit,
-               plan_score, plan_score_calls, plan_score_layers, plan_score_per_layer, plan_sparse_verify_attn,
-               plan_sparse_verify_attn_kv4, plan_topk, topk, verify_tokens)
+from . import (KV4, TOPK_MAX_LEN, digit_hist, kv4_append, kv4_empty, kv_evict, plan_kv4_append, plan_kv_append,
+               plan_kv_commit, plan_score, plan_score_calls, plan_score_layers, plan_score_per_layer,
+               plan_sparse_verify_attn, plan_sparse_verify_attn_kv4, plan_topk, topk, verify_tokens)
 
 
 def window_kv(s, layer) -> tuple:
@@ -157,7 +157,10 @@ class VerifyStep:
         estimation's arrays over the positions (a history, given draft scores) and the lengths follow.  Behind the kept
         positions these arrays are zero: positions to come have no history.  Returns (idx, count)."""
         s, first = self.s, self.layers[0]
-        idx, cnt = topk(None, weights, self.seq, keep, n_sink=s.n_sink, n_window=s.n_window)
+        # accepted tokens may lie past the weights' end: without a weight, but as positions (the most recent ones)
+        missing = min(s.n_max + s.t_max, TOPK_MAX_LEN) - weights.shape[2]
+        ranked = torch.nn.functional.pad(weights, (0, missing)) if missing > 0 else weights
+        idx, cnt = topk(None, ranked, self.seq, keep, n_sink=s.n_sink, n_window=s.n_window)
         arrays = {x.data_ptr(): x for x in (weights, self.est.init_target, self.est.s_draft_given) if x is not None}
         for x in arrays.values():
             self._cut(x, idx, cnt)

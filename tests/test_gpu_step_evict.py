@@ -88,6 +88,25 @@ def test_the_step_after_an_eviction(name, by, captured):
         assert st.seq.tolist() == lens
 
 
+def test_tokens_accepted_past_the_weights_end_stay():
+    """The step's scores end at its longest context; the tokens accepted after them are the most recent positions."""
+    s, layers, est = build("history")
+    st = S.VerifyStep(s, layers, est, DEV)
+    st.run()
+    st.commit(st.nq)
+    torch.cuda.synchronize()
+    keys = [l.k.clone() for l in layers]
+    idx, cnt = st.evict(st.s_t, 150)
+    torch.cuda.synchronize()
+    assert cnt.view(-1).tolist() == st.seq.tolist() == [150, 150]
+    for b, (n, t) in enumerate(zip(s.seq_lens, s.n_query)):
+        recent = list(range(n + t - s.n_window, n + t))
+        assert idx[b, 0, 150 - s.n_window:150].tolist() == recent
+        for k, l in zip(keys, layers):
+            assert torch.equal(l.k[b, 150 - s.n_window:150].view(torch.int16), k[b, recent].view(torch.int16))
+        assert (st.s_t[b, 0, 150 - t:] == 0).all() or n < s.n_max  # (past the end: no weight yet)
+
+
 def test_weights_alone():
     """Arrays over the positions without a cache, to others and in place, several groups."""
     g = torch.Generator(device=DEV).manual_seed(1)

@@ -106,6 +106,11 @@ __device__ __forceinline__ uint32_t pk_bf16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
 }
 
+// c + the sum of two packed bf16 numbers.
+__device__ __forceinline__ float add_bf16(uint32_t two, float c) {
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), __builtin_bit_cast(bf16x2, 0x3f803f80u), c, false);
+}
+
 // floor(a / b) for 0 <= a < 2^22, 1 <= b < 2^22: the reciprocal's estimate is within one of it.
 __device__ __forceinline__ int div22(int a, int b) {
   int q = (int)((float)a * __builtin_amdgcn_rcpf((float)b));
@@ -369,8 +374,10 @@ __global__ __launch_bounds__(kThreads4, RT <= kAttn4Two ? 4 : 2) void attn_kv4_k
       float p[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) p[e] = fast_exp2(fmaf(sc[rt][e], a.scale_log2, -m_ref[rt]));
+      // bf16 operands, as the bf16 caches' attention has them; the sum is of what they are rounded to, so that an output
+      // is a weighted mean of values to within 32-bit arithmetic
       p_op[rt] = u32x2{pk_bf16(p[0], p[1]), pk_bf16(p[2], p[3])};
-      p_sum[rt] = (p[0] + p[1]) + (p[2] + p[3]);
+      p_sum[rt] = add_bf16(p_op[rt][0], add_bf16(p_op[rt][1], 0.f));
     };
     auto own_max = [&](int rt) {
       return fmaxf(fmaxf(sc[rt][0], sc[rt][1]), fmaxf(sc[rt][2], sc[rt][3])) * a.scale_log2;

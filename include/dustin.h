@@ -545,8 +545,8 @@ dustin_status dustin_kv4_read(void* k_out, int64_t k_sb, int64_t k_st, int64_t k
  *   - with n_query, the caches must address max_len positions alone (as dustin_kv4_append);
  *   - the caches' rows may lie anywhere a 64-bit offset reaches, pages need not be packed; strides of positions and of
  *     pages (data's and the scales') are below 2^32 bytes, and max_len and k_max at most 2^31 - 4097;
- *   - workspace: dustin_attn_kv4_workspace(...) bytes, 256-byte aligned, of any content.  Calls that share a
- *     workspace must not overlap.
+ *   - workspace: dustin_attn_kv4_workspace(...) bytes, 256-byte aligned, of any content; one for the largest batch,
+ *     window and token count serves all smaller calls.  Calls that share a workspace must not overlap.
  * max_tokens of the workspace is k_max (sparse) or max_len (dense).  batch * num_kv_heads <= 65536, and the granules of
  * 128 tokens that max_tokens + nq_max come to, over all of them, at most 2^30.
  * --------------------------------------------------------------------------------- */

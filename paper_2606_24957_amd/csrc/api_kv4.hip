@@ -129,6 +129,13 @@ Attn4Ws attn4_ws(int64_t pairs, int units, int64_t rows_max) {
   w.total = w.acc + round_up((size_t)units * 2 * rows_max * 128 * sizeof(float), kAlign);
   return w;
 }
+// What a call asks for: enough for any with fewer rows, too, which may have more runs.
+size_t attn4_ws_bytes(int64_t pairs, int64_t tokens, int64_t rows) {
+  const size_t own = attn4_ws(pairs, attn4_units(pairs, tokens, rows), rows).total;
+  const int64_t two = rows < 16 * kAttn4Two ? rows : 16 * kAttn4Two;
+  const size_t fewer = attn4_ws(pairs, attn4_units(pairs, tokens, two), two).total;
+  return own > fewer ? own : fewer;
+}
 
 dustin_status attn4(bool sparse, const void* q, int64_t q_sb, int64_t q_st, int64_t q_sh, int32_t num_q_heads,
                     const dustin_kv4* k, const dustin_kv4* v, const dustin_batch* bt, const int32_t* idx,
@@ -188,7 +195,7 @@ dustin_status attn4(bool sparse, const void* q, int64_t q_sb, int64_t q_st, int6
   a.rows_max = bt->nq_max * gs;
   a.units = attn4_units(pairs, tokens, a.rows_max);
   const Attn4Ws w = attn4_ws(pairs, a.units, a.rows_max);
-  if (!ws || ws_bytes < w.total || !aligned(ws, kAlign)) return DUSTIN_ERR_WORKSPACE;
+  if (!ws || ws_bytes < attn4_ws_bytes(pairs, tokens, a.rows_max) || !aligned(ws, kAlign)) return DUSTIN_ERR_WORKSPACE;
   char* base = static_cast<char*>(ws);
   a.plan = reinterpret_cast<int32_t*>(base);
   a.part_ml = reinterpret_cast<float2*>(base + w.ml);
@@ -313,7 +320,7 @@ size_t dustin_attn_kv4_workspace(int32_t batch, int32_t num_q_heads, int32_t num
     return 0;
   const int64_t pairs = (int64_t)batch * num_kv_heads;
   const int64_t rows = (int64_t)nq_max * (num_q_heads / num_kv_heads);
-  return attn4_ws(pairs, attn4_units(pairs, (int64_t)max_tokens + nq_max, rows), rows).total;
+  return attn4_ws_bytes(pairs, (int64_t)max_tokens + nq_max, rows);
 }
 
 dustin_status dustin_sparse_verify_attn_kv4(const void* q, int64_t q_sb, int64_t q_st, int64_t q_sh,

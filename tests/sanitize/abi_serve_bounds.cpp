@@ -108,6 +108,19 @@ int main() {
     EXPECT(dustin::attn_args.k.capacity, 104);
     EXPECT(dustin::attn_args.v.capacity, 104);
   }
+  // ---- the workspace of a larger call serves a smaller one: fewer rows, sequences or tokens
+  for (const int gs : {1, 4, 7, 8})
+    for (const int B : {1, 9, 300})
+      for (const int n : {0, 1, 500, 4000}) {
+        const dustin_kv4 k = kv4(5000), v = kv4(5000, 1 << 20);
+        for (int nq = 2; nq * gs <= 128; ++nq) {
+          const size_t bytes = dustin_attn_kv4_workspace(B, 2 * gs, 2, nq, n);
+          EXPECT(attn(false, k, v, batch(B, n, nq, false), 2 * gs, bytes), PASSED);
+          EXPECT(attn(false, k, v, batch(B, n, nq - 1, false), 2 * gs, bytes), PASSED);
+          EXPECT(attn(false, k, v, batch((B + 1) / 2, n / 2, (nq + 1) / 2, false), 2 * gs, bytes), PASSED);
+          EXPECT(attn(false, k, v, batch(B, n, nq, false), 2 * gs, bytes - 1), DUSTIN_ERR_WORKSPACE);
+        }
+      }
   // ---- eviction of weights without a cache
   {
     auto alone = [&](const float* w, float* wo, int groups, int w_len, const int32_t* count) {

@@ -493,7 +493,8 @@ dustin_status dense_verify_attn(const void* q, int64_t q_sb, int64_t q_st, int64
  *   k_new, v_new  bf16 [B, nq_max, Hkv, d] (strides *_sb, *_st, *_sh in elements, inner
  *       stride 1, 16-byte aligned rows); read only for t < T_b
  *   k, v          the caches (as for the attention; d a multiple of 8; one page table);
- *                 must address max_len + nq_max positions per sequence
+ *                 must address max_len + nq_max positions per sequence.  v and v_new NULL:
+ *                 a cache of keys alone (as the scores read)
  *   bt            seq_lens (N_b), n_query (T_b, NULL = nq_max), max_len, nq_max
  * Device arrays are read on the stream; nothing is read back on the host.
  * --------------------------------------------------------------------------------- */

@@ -823,23 +823,25 @@ def dense_verify_attn(q, k, v, seq_lens, **kw):
 
 # ----------------------------------------------------------------------------- KV append / commit
 
-def plan_kv_append(k_new: torch.Tensor, v_new: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+def plan_kv_append(k_new: torch.Tensor, v_new: Optional[torch.Tensor], k: torch.Tensor, v: Optional[torch.Tensor],
                    seq_lens, *, n_query=None, page_table: Optional[torch.Tensor] = None,
                    max_len: Optional[int] = None, stream=None) -> Call:
     """Prepared dustin_kv_append: k_new / v_new bf16 [B, T_max, Hkv, d] go to cache
-    positions [N_b, N_b + T_b) of k / v (contiguous [B, N_cap, Hkv, d] or paged)."""
+    positions [N_b, N_b + T_b) of k / v (contiguous [B, N_cap, Hkv, d] or paged).  v_new and v None: k alone."""
     _on_gpu(k_new, v_new, k, v, page_table)
     B, nq_max = k_new.shape[0], k_new.shape[1]
     dev = k_new.device
-    kv, vv = kv_view(k, page_table), kv_view(v, page_table)
+    if (v is None) != (v_new is None):
+        raise ValueError("v_new goes with v")
+    kv, vv = kv_view(k, page_table), None if v is None else kv_view(v, page_table)
     if max_len is None:
         max_len = _capacity(kv) - nq_max
     seq = _i32_dev(seq_lens, dev)
     nqa = _i32_dev(n_query, dev)
     bt = _batch(B, max_len, nq_max, 0, seq, nqa)
     args = (_ptr(k_new), k_new.stride(0), k_new.stride(1), k_new.stride(2), _ptr(v_new),
-            v_new.stride(0), v_new.stride(1), v_new.stride(2), ctypes.byref(kv), ctypes.byref(vv),
-            ctypes.byref(bt), _stream(stream))
+            *((0, 0, 0) if v is None else v_new.stride()[:3]), ctypes.byref(kv),
+            None if v is None else ctypes.byref(vv), ctypes.byref(bt), _stream(stream))
     return Call(lib().dustin_kv_append, args, "dustin_kv_append", (k_new, v_new, k, v, kv, vv, bt), None)
 
 

@@ -1085,21 +1085,22 @@ dustin_status dustin_kv_append(const void* k_new, int64_t k_sb, int64_t k_st, in
                                const void* v_new, int64_t v_sb, int64_t v_st, int64_t v_sh,
                                const dustin_kv* k, const dustin_kv* v, const dustin_batch* bt,
                                void* stream) {
-  if (!batch_ok(bt) || !k_new || !v_new || !k || !v) return DUSTIN_ERR_INVALID_ARG;
+  if (!batch_ok(bt) || !k_new || !k || !v_new != !v) return DUSTIN_ERR_INVALID_ARG;
   if (bt->batch == 0 || bt->nq_max == 0) return DUSTIN_OK;
   const int d = k->head_dim, H = k->num_kv_heads;
-  if (d <= 0 || d % 8 || v->head_dim != d || v->num_kv_heads != H || H <= 0) return DUSTIN_ERR_INVALID_ARG;
-  if (k->page_table != v->page_table) return DUSTIN_ERR_INVALID_ARG;
-  if (!rows_aligned(k_new, k_sb, k_st, k_sh) || !rows_aligned(v_new, v_sb, v_st, v_sh))
+  if (d <= 0 || d % 8 || H <= 0) return DUSTIN_ERR_INVALID_ARG;
+  if (v && (v->head_dim != d || v->num_kv_heads != H || k->page_table != v->page_table)) return DUSTIN_ERR_INVALID_ARG;
+  if (!rows_aligned(k_new, k_sb, k_st, k_sh) || (v && !rows_aligned(v_new, v_sb, v_st, v_sh)))
     return DUSTIN_ERR_INVALID_ARG;
-  if (k_sb < 0 || k_st < 0 || k_sh < 0 || v_sb < 0 || v_st < 0 || v_sh < 0) return DUSTIN_ERR_INVALID_ARG;
+  if (k_sb < 0 || k_st < 0 || k_sh < 0 || (v && (v_sb < 0 || v_st < 0 || v_sh < 0))) return DUSTIN_ERR_INVALID_ARG;
   KvAppendArgs a;
   memset(&a, 0, sizeof a);
   const int64_t need = (int64_t)bt->max_len + bt->nq_max;
   dustin_status st = kv_of(k, d, need, &a.k);
   if (st != DUSTIN_OK) return st;
-  st = kv_of(v, d, need, &a.v);
+  if (v) st = kv_of(v, d, need, &a.v);
   if (st != DUSTIN_OK) return st;
+  a.caches = v ? 2 : 1;
   a.k_new = static_cast<const uint16_t*>(k_new);
   a.k_sb = k_sb;
   a.k_st = k_st;

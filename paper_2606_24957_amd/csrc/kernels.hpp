@@ -281,6 +281,7 @@ struct KvAppendArgs {
   const uint16_t* v_new;
   int64_t v_sb, v_st, v_sh;
   KvView k, v;   // the caches (written)
+  int32_t caches;  // 2, or 1: K alone
   SeqDims dims;  // seq_lens (N_b), n_query (T_b), max_len, nq_max
   int32_t batch, num_kv_heads, head_dim;
 };

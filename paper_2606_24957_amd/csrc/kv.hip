@@ -14,8 +14,9 @@ constexpr int kKvThreads = 256;
 // Bound by its launch and chain of loads (lengths, page, row): with the row found by 64-bit divisions,
 // 3.9 to 4.8 us a launch for one sequence, 5 rows of 8 KV heads, about 0.5 us more than now.
 __global__ __launch_bounds__(kKvThreads) void kv_append_kernel(KvAppendArgs a, uint32_t parts, int b0) {
-  const bool is_v = blockIdx.x & 1;
-  const uint32_t seq = (blockIdx.x >> 1) / parts, part = (blockIdx.x >> 1) - seq * parts;
+  const uint32_t both = (uint32_t)a.caches - 1, blk = blockIdx.x >> both;
+  const bool is_v = blockIdx.x & both;
+  const uint32_t seq = blk / parts, part = blk - seq * parts;
   const int b = b0 + (int)seq;
   const int T = a.dims.nq(b), N = a.dims.len(b);
   const uint32_t cpr = (uint32_t)a.head_dim / 8, heads = (uint32_t)a.num_kv_heads;  // chunks per row
@@ -45,11 +46,11 @@ hipError_t launch_kv_append(const KvAppendArgs& a, hipStream_t stream) {
   const int64_t chunks = (int64_t)a.dims.nq_max * a.num_kv_heads * (a.head_dim / 8);  // of one sequence
   if (a.batch == 0 || chunks == 0) return hipSuccess;
   const int64_t parts = (chunks + kKvThreads - 1) / kKvThreads;
-  const int64_t most = ((INT64_C(1) << 32) / kKvThreads - 1) / (2 * parts);  // sequences: a grid has less than 2^32 threads
+  const int64_t most = ((INT64_C(1) << 32) / kKvThreads - 1) / (a.caches * parts);  // sequences: a grid has less than 2^32 threads
   if (most < 1) return hipErrorInvalidValue;
   for (int64_t b0 = 0; b0 < a.batch; b0 += most) {
     const int64_t n = a.batch - b0 < most ? a.batch - b0 : most;
-    hipLaunchKernelGGL(kv_append_kernel, dim3((unsigned)(2 * n * parts)), dim3(kKvThreads), 0, stream, a,
+    hipLaunchKernelGGL(kv_append_kernel, dim3((unsigned)(a.caches * n * parts)), dim3(kKvThreads), 0, stream, a,
                        (uint32_t)parts, (int)b0);
   }
   return hipGetLastError();

@@ -103,8 +103,7 @@ class VerifyStep:
                              n_sink=s.n_sink, n_window=s.n_window, groups=s.groups, idx=self.idx,
                              count=self.cnt, hist_d=self.hist_d, hist_t=self.hist_t, stream=stream))
         if self.append and self.score_k is not self.layers[0].k:
-            k_new = self.windows[0][0]  # (keys alone: the append's two halves write the same rows)
-            ops.append(plan_kv_append(k_new, k_new, self.score_k, self.score_k, self.seq, n_query=self.nq,
+            ops.append(plan_kv_append(self.windows[0][0], None, self.score_k, None, self.seq, n_query=self.nq,
                                       page_table=self.layers[0].page_table, max_len=N, stream=stream))
         for L, o, (k_new, v_new) in zip(self.layers, self.outs, self.windows):
             if self.append:

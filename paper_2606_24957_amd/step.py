@@ -46,6 +46,11 @@ def layer4(s, layer):
     return dataclasses.replace(layer, k=k, v=v)
 
 
+def _place(cache) -> int:
+    """Where a cache lies: views of one cache are that cache."""
+    return (cache.data if isinstance(cache, KV4) else cache).data_ptr()
+
+
 def _plan_sparse(layer):
     """The sparse attention of the layer's kind of cache."""
     return plan_sparse_verify_attn_kv4 if isinstance(layer.k, KV4) else plan_sparse_verify_attn
@@ -102,7 +107,7 @@ class VerifyStep:
         ops.append(plan_topk(self.s_d, self.s_t, self.seq, s.k_max, budget=self.bud, m=self.mm,
                              n_sink=s.n_sink, n_window=s.n_window, groups=s.groups, idx=self.idx,
                              count=self.cnt, hist_d=self.hist_d, hist_t=self.hist_t, stream=stream))
-        if self.append and self.score_k is not self.layers[0].k:
+        if self.append and _place(self.score_k) != _place(self.layers[0].k):
             ops.append(plan_kv_append(self.windows[0][0], None, self.score_k, None, self.seq, n_query=self.nq,
                                       page_table=self.layers[0].page_table, max_len=N, stream=stream))
         for L, o, (k_new, v_new) in zip(self.layers, self.outs, self.windows):
@@ -163,13 +168,20 @@ class VerifyStep:
         arrays = {x.data_ptr(): x for x in (weights, self.est.init_target, self.est.s_draft_given) if x is not None}
         for x in arrays.values():
             self._cut(x, idx, cnt)
-        kv_evict(first.k, first.v, idx, cnt, page_table=first.page_table, new_lens=self.seq)
+        done = set()
+
+        def once(k, v, page_table, **kw):  # (layers, the scores and a draft model may share caches)
+            new = {_place(x): x for x in (k, v) if x is not None and _place(x) not in done}
+            done.update(new)
+            if new:
+                kv_evict(*(*new.values(), None)[:2], idx, cnt, page_table=page_table, **kw)
+
+        once(first.k, first.v, first.page_table, new_lens=self.seq)
         for L in self.layers[1:]:
-            kv_evict(L.k, L.v, idx, cnt, page_table=L.page_table)
-        if self.score_k is not first.k:
-            kv_evict(self.score_k, None, idx, cnt, page_table=first.page_table)
+            once(L.k, L.v, L.page_table)
+        once(self.score_k, None, first.page_table)
         for k in self.est.draft_k:
-            kv_evict(k, None, idx, cnt)
+            once(k, None, None)
         return idx, cnt
 
     @staticmethod

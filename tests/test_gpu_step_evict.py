@@ -107,6 +107,28 @@ def test_tokens_accepted_past_the_weights_end_stay():
         assert (st.s_t[b, 0, 150 - t:] == 0).all() or n < s.n_max  # (past the end: no weight yet)
 
 
+def test_caches_that_share_memory_are_cut_once():
+    """A second view of the scoring keys, a layer that has another's keys, a draft layer that reads a target layer's."""
+    s, layers, est = build("history")
+    two = [layers[0], W.Layer(layers[1].q, layers[0].k[:], layers[1].v)]
+    draft = [est.draft_k[0], layers[0].k[:], est.draft_k[0].view(est.draft_k[0].shape)]
+    shared = W.Estimation(est.q_target, est.init_target, None, est.draft_q, draft)
+    st = S.VerifyStep(s.replace(draft=None), two, W.Estimation(est.q_target, est.init_target, torch.rand_like(est.init_target)),
+                      DEV, windows=[S.window_kv(s, l) for l in layers], score_k=layers[0].k.view(layers[0].k.shape))
+    st.est = shared
+    held = [layers[0].k, layers[0].v, layers[1].v, draft[0]]
+    old = [x.clone() for x in held]
+    idx, cnt = st.evict(torch.rand((s.B, 1, s.n_max), device=DEV), 150)
+    torch.cuda.synchronize()
+    for x, y in zip(held, old):
+        for b in range(s.B):
+            at = idx[b, 0, :int(cnt[b, 0])].long()
+            assert torch.equal(x[b, :len(at)].view(torch.int16), y[b, at].view(torch.int16))
+            assert torch.equal(x[b, len(at):].view(torch.int16), y[b, len(at):].view(torch.int16))
+    # and the scoring keys of a second view are not appended by themselves
+    assert len(st.ops) == 2 + 1 + 2 * len(layers)
+
+
 def test_weights_alone():
     """Arrays over the positions without a cache, to others and in place, several groups."""
     g = torch.Generator(device=DEV).manual_seed(1)

@@ -521,7 +521,8 @@ dustin_status dustin_kv_commit(int32_t* seq_lens, const int32_t* accepted, const
  * beyond 6.  An infinity counts as the largest finite bf16 of its sign, a NaN as zero.
  *   k_new, v_new  bf16 [B, nq_max, Hkv, d] (d 64 or 128), strides in elements, as dustin_kv_append
  *   k, v          the caches; must address max_len + nq_max positions per sequence, with n_query max_len: then a sequence
- *                 needs room (pages) for its own N_b + T_b alone; rows past a cache's end are not written
+ *                 needs room (pages) for its own N_b + T_b alone; rows past a cache's end are not written.  Sequences and heads
+ *                 have places of their own (no stride of zero between them)
  *   bt            seq_lens (N_b), n_query (T_b, NULL = nq_max), max_len, nq_max
  * --------------------------------------------------------------------------------- */
 dustin_status dustin_kv4_append(const void* k_new, int64_t k_sb, int64_t k_st, int64_t k_sh, const void* v_new,
@@ -578,11 +579,13 @@ dustin_status dustin_dense_verify_attn_kv4(const void* q, int64_t q_sb, int64_t 
  *       equal data, strides and page tables mark the call as in place.  Caches that overlap in another way are not
  *       supported, nor is one of K and V in place alone (DUSTIN_ERR_INVALID_ARG).  k_out and v_out address at least
  *       k_max positions.  v and v_out may be NULL (a cache of keys alone, as the scores read); one cache must not be
- *       given as both k and v, and a page that two sequences share must not be written.
+ *       given as both k and v, and a page that two sequences share must not be written (a stride of zero between
+ *       sequences or heads of k_out or v_out: DUSTIN_ERR_INVALID_ARG).
  *   idx, count  int32 [B, groups, >= k_max] (strides idx_sb, idx_sg) and [B * groups]; ascending positions (in place,
  *       others give rows of unspecified content); a position outside
  *       the cache counts as its nearest end; groups 1 or the KV head count
- *   w, w_out    fp32 [B, groups, >= w_len], [B, groups, >= k_max] (strides in elements) or both NULL; w_out may be w
+ *   w, w_out    fp32 [B, groups, >= w_len], [B, groups, >= k_max] (strides in elements) or both NULL; w_out may be w, with
+ *               w's strides
  *   new_lens    int32 [B] or NULL; may be the batch's seq_lens, which this call does not read
  * A step's layers share idx: pass w and new_lens with one of them.  Without any cache (k, v, k_out and v_out NULL) the
  * weights alone are moved, for any number of groups: other arrays over the same positions, such as a history.

@@ -1150,6 +1150,8 @@ def plan_kv_evict(k, v, idx: torch.Tensor, count: torch.Tensor, *, k_out=None, v
             raise ValueError(f"weights_out {tuple(weights_out.shape)} does not hold [{B}, {G}, {k_max}]")
         ws = (weights.stride(0), weights.stride(1) if weights.shape[1] > 1 else 0, n, weights_out.stride(0),
               weights_out.stride(1))
+        if weights.data_ptr() == weights_out.data_ptr() and ((B > 1 and ws[0] != ws[3]) or (G > 1 and ws[1] != ws[4])):
+            raise ValueError("weights_out lies where weights do, with rows of another length")
     if new_lens is not None and (new_lens.dtype != torch.int32 or new_lens.numel() < B or not new_lens.is_contiguous()):
         raise ValueError("new_lens must be a contiguous int32 [B] tensor")
     what = "dustin_kv4_evict" if four else "dustin_kv_evict"

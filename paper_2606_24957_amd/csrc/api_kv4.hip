@@ -70,6 +70,16 @@ bool same_layout(const Kv* k, const Kv* v) {
           (k->page_size == v->page_size && k->max_pages == v->max_pages && k->num_pages == v->num_pages));
 }
 
+// Rows written for several sequences, or heads, have places of their own (with pages, the table says so).
+template <class Kv>
+bool apart(const Kv* c, int batch) {
+  return (c->num_kv_heads <= 1 || c->stride_h > 0) && (batch <= 1 || c->page_table || c->stride_b > 0);
+}
+bool apart(const dustin_kv4* c, int batch) {
+  return apart<dustin_kv4>(c, batch) && (c->num_kv_heads <= 1 || c->scale_stride_h > 0) &&
+         (batch <= 1 || c->page_table || c->scale_stride_b > 0);
+}
+
 dustin_status kv4_rows(bool append, const void* k_rows, int64_t k_sb, int64_t k_st, int64_t k_sh, const void* v_rows,
                        int64_t v_sb, int64_t v_st, int64_t v_sh, const dustin_kv4* k, const dustin_kv4* v,
                        const dustin_batch* bt, void* stream) {
@@ -77,7 +87,7 @@ dustin_status kv4_rows(bool append, const void* k_rows, int64_t k_sb, int64_t k_
   const bool none = bt->batch == 0 || bt->nq_max == 0;  // no rows: they may lie nowhere
   if (!none && (!k_rows || !v_rows)) return DUSTIN_ERR_INVALID_ARG;
   if (!rows_aligned(k_rows, k_sb, k_st, k_sh) || !rows_aligned(v_rows, v_sb, v_st, v_sh)) return DUSTIN_ERR_INVALID_ARG;
-  if (!same_layout(k, v)) return DUSTIN_ERR_INVALID_ARG;
+  if (!same_layout(k, v) || (append && (!apart(k, bt->batch) || !apart(v, bt->batch)))) return DUSTIN_ERR_INVALID_ARG;
   Kv4RowsArgs a;
   memset(&a, 0, sizeof a);
   const int64_t need = positions_of(bt);
@@ -255,6 +265,7 @@ dustin_status evict(const Kv* k, const Kv* v, const Kv* k_out, const Kv* v_out, 
                k->head_dim != k_out->head_dim))
     return DUSTIN_ERR_INVALID_ARG;
   if (v && (k->data == v->data || k_out->data == v_out->data)) return DUSTIN_ERR_INVALID_ARG;
+  if (rows && (!apart(k_out, batch) || (v_out && !apart(v_out, batch)))) return DUSTIN_ERR_INVALID_ARG;
   if (rows ? groups != 1 && groups != k->num_kv_heads : groups < 1) return DUSTIN_ERR_INVALID_ARG;
   if (!aligned(idx, 4) || !aligned(count, 4) || !aligned(new_lens, 4) || idx_sb < 0 || idx_sg < 0)
     return DUSTIN_ERR_INVALID_ARG;

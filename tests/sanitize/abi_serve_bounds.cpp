@@ -140,6 +140,34 @@ int main() {
                             200, 40, 200, at<float>(), 200, 40, nullptr, nullptr),
            BAD);
   }
+  // ---- rows of several sequences or heads are not written to one place
+  {
+    dustin_kv4 k = kv4(200), v = kv4(200, 1 << 20), ko = kv4(200, 2 << 20), vo = kv4(200, 3 << 20);
+    auto evict = [&](const dustin_kv4& a, const dustin_kv4& b, const dustin_kv4& c, const dustin_kv4& d, int B = 2) {
+      return (int)dustin_kv4_evict(&a, &b, &c, &d, B, at<int32_t>(), 40, 40, at<int32_t>(), 1, 40, nullptr, 0, 0, 0, nullptr,
+                                   0, 0, nullptr, nullptr);
+    };
+    EXPECT(evict(k, v, ko, vo), PASSED);
+    for (int what = 0; what < 4; ++what) {
+      dustin_kv4 x = ko;
+      int64_t* const stride[4] = {&x.stride_b, &x.scale_stride_b, &x.stride_h, &x.scale_stride_h};
+      *stride[what] = 0;
+      EXPECT(evict(k, v, x, vo), BAD);
+      dustin_kv4 y = x;
+      y.data = y.scales = fake(4 << 20);
+      EXPECT(evict(y, v, ko, vo), PASSED);  // (read, they may be)
+      EXPECT(evict(x, v, x, v), BAD);
+      EXPECT(evict(k, v, x, vo, 1), what < 2 ? PASSED : BAD);
+      EXPECT(rows(true, x, vo, batch(2, 100, 4, false)), BAD);
+      EXPECT(rows(true, k, x, batch(2, 100, 4, false)), BAD);
+      EXPECT(rows(true, x, vo, batch(1, 100, 4, false)), what < 2 ? PASSED : BAD);
+      EXPECT(rows(false, x, vo, batch(2, 100, 4, false)), PASSED);
+    }
+    dustin_kv4 p = paged4(7, 2 << 20), q = paged4(7, 3 << 20);
+    p.stride_b = p.scale_stride_b = q.stride_b = q.scale_stride_b = 0;  // (not used)
+    EXPECT(evict(p, q, p, q), PASSED);
+    EXPECT(rows(true, p, q, batch(2, 100, 4, false)), PASSED);
+  }
   printf("%s: %d failed expectations\n", failures ? "FAILED" : "ok", failures);
   return failures ? 1 : 0;
 }

@@ -155,3 +155,28 @@ def test_weights_alone():
         D.kv_evict(None, None, idx, cnt, new_lens=lens)
     with pytest.raises(ValueError, match="only weights"):
         D.kv_evict(None, None, idx, cnt, weights=w, k_out=out)
+
+
+def test_weights_are_not_written_over_rows_still_to_be_read():
+    w = torch.rand((2, 3, 500), device=DEV)
+    idx = torch.arange(100, 140, dtype=torch.int32, device=DEV).expand(2, 3, 40).contiguous()
+    cnt = torch.full((2, 3), 40, dtype=torch.int32, device=DEV)
+    dense = w.view(-1)[:240].view(2, 3, 40)
+    with pytest.raises(ValueError, match="another length"):
+        D.kv_evict(None, None, idx, cnt, weights=w, weights_out=dense)
+    with pytest.raises(ValueError, match="another length"):
+        D.kv_evict(None, None, idx[:, :1], cnt[:, :1], weights=w[:, :1], weights_out=dense[:, :1])
+    want = w[:, :, 100:140].clone()
+    D.kv_evict(None, None, idx, cnt, weights=w, weights_out=w[:, :, :200])  # its own rows
+    assert torch.equal(w[:, :, :40], want)
+    D.kv_evict(None, None, idx[:1, :1], cnt[:1, :1], weights=w, weights_out=dense)  # one row
+    torch.cuda.synchronize()
+
+
+def test_sequences_of_one_cache_are_not_cut_in_place():
+    k = torch.zeros((1, 64, 2, 128), dtype=torch.bfloat16, device=DEV)
+    idx, cnt = torch.arange(8, 16, dtype=torch.int32, device=DEV).expand(3, 1, 8).contiguous(), torch.full((3, 1), 8, dtype=torch.int32, device=DEV)
+    with pytest.raises(D.DustinError):
+        D.kv_evict(k.expand(3, 64, 2, 128), None, idx, cnt)
+    D.kv_evict(k.expand(3, 64, 2, 128), None, idx, cnt, k_out=torch.empty((3, 8, 2, 128), dtype=torch.bfloat16, device=DEV))
+    torch.cuda.synchronize()

@@ -289,6 +289,8 @@ dustin_status evict(const Kv* k, const Kv* v, const Kv* k_out, const Kv* v_out, 
     a.row_bytes = k->head_dim * row_bytes_per_dim2 / 2;
     a.scale_bytes = four ? k->head_dim / kKv4Block : 0;
     a.in_place = same_k;
+    // (32-bit counts of a sequence's pieces)
+    if (!same_k && (int64_t)k_max * a.num_kv_heads * a.caches * (a.row_bytes / 16) > INT32_MAX) return DUSTIN_ERR_UNSUPPORTED;
   }
   if (batch == 0) return DUSTIN_OK;
   a.idx = idx;

@@ -52,14 +52,13 @@ __device__ __forceinline__ void evict_weights(const EvictArgs& a, int row) {
 // While each thread also carried the addresses of several chunks it took 22.8; with 2, 4 and 8 chunks to a thread, loaded before the first is stored, 24.8, 27.1 and 36.2: the more workgroups, the
 // more of one's loads run beside another's stores.  Stores past the caches: 27.3.
 template <int CPR>  // 16-byte chunks of a row
-__global__ __launch_bounds__(kEvictThreads) void evict_kernel(EvictArgs a, uint32_t parts, uint32_t extra) {
+__global__ __launch_bounds__(kEvictThreads) void evict_kernel(EvictArgs a, uint32_t parts, uint32_t extra, int b0) {
   if (blockIdx.x < extra) {
     evict_weights(a, (int)blockIdx.x);
     return;
   }
-  const uint32_t blk = blockIdx.x - extra;
-  const int b = (int)(blk / parts);
-  const uint32_t part = blk - (uint32_t)b * parts;
+  const uint32_t blk = blockIdx.x - extra, seq = blk / parts, part = blk - seq * parts;
+  const int b = b0 + (int)seq;
   const uint32_t H = (uint32_t)a.num_kv_heads;
   const uint32_t e = part * kEvictThreads + threadIdx.x;
   const uint32_t chunk = e % CPR, r = a.caches == 2 ? e / (2 * CPR) : e / CPR;
@@ -147,24 +146,28 @@ __global__ __launch_bounds__(kEvictRunThreads) void evict_in_place_kernel(EvictA
 hipError_t launch_evict(const EvictArgs& a, hipStream_t stream) {
   const int64_t extra = a.w || a.new_lens ? (int64_t)a.batch * a.groups : 0;
   const int cpr = a.row_bytes / 16;
-  int64_t grid;
   if (a.in_place) {
     const int sch = cpr < 4 ? cpr : 4;
     const int64_t slices = cpr / sch;
-    grid = extra + a.caches * (int64_t)a.batch * a.num_kv_heads * slices;
+    const int64_t grid = extra + a.caches * (int64_t)a.batch * a.num_kv_heads * slices;
     if (grid > INT32_MAX / kEvictRunThreads) return hipErrorInvalidValue;
     if (grid == 0) return hipSuccess;
     hipLaunchKernelGGL(sch == 4 ? evict_in_place_kernel<4> : evict_in_place_kernel<2>, dim3((unsigned)grid),
                        dim3(kEvictRunThreads), 0, stream, a, (uint32_t)slices, (uint32_t)extra);
     return hipGetLastError();
   }
-  const int64_t chunks = (int64_t)a.k_max * a.num_kv_heads * a.caches * cpr;
+  const int64_t chunks = (int64_t)a.k_max * a.num_kv_heads * a.caches * cpr;  // of one sequence
   const int64_t parts = (chunks + kEvictThreads - 1) / kEvictThreads;
-  grid = extra + parts * a.batch;
-  if (grid > INT32_MAX / kEvictThreads || chunks > INT32_MAX) return hipErrorInvalidValue;
-  if (grid == 0) return hipSuccess;
+  const int64_t room = (INT64_C(1) << 32) / kEvictThreads - 1 - extra;  // a grid has less than 2^32 threads
+  if (room < parts) return hipErrorInvalidValue;
   auto kernel = cpr == 2 ? evict_kernel<2> : cpr == 4 ? evict_kernel<4> : cpr == 8 ? evict_kernel<8> : evict_kernel<16>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kEvictThreads), 0, stream, a, (uint32_t)parts, (uint32_t)extra);
+  const int64_t most = parts ? room / parts : a.batch;  // sequences
+  for (int64_t b0 = 0; b0 < a.batch; b0 += most) {
+    const int64_t n = a.batch - b0 < most ? a.batch - b0 : most, first = b0 == 0 ? extra : 0;
+    if (first + n * parts == 0) continue;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(first + n * parts)), dim3(kEvictThreads), 0, stream, a, (uint32_t)parts,
+                       (uint32_t)first, (int)b0);
+  }
   return hipGetLastError();
 }
 

@@ -168,6 +168,16 @@ int main() {
     EXPECT(evict(p, q, p, q), PASSED);
     EXPECT(rows(true, p, q, batch(2, 100, 4, false)), PASSED);
   }
+  {  // ---- the most that one sequence may move to other caches
+    dustin_kv4 k = paged4(1 << 24), v = paged4(1 << 24, 1 << 20), ko = paged4(1 << 24, 2 << 20), vo = paged4(1 << 24, 3 << 20);
+    auto evict = [&](bool in_place, int k_max) {
+      return (int)dustin_kv4_evict(&k, &v, in_place ? &k : &ko, in_place ? &v : &vo, 2, at<int32_t>(), 40, 40, at<int32_t>(), 1,
+                                   k_max, nullptr, 0, 0, 0, nullptr, 0, 0, nullptr, nullptr);
+    };
+    EXPECT(evict(false, (1 << 27) - 1), PASSED);
+    EXPECT(evict(false, 1 << 27), DUSTIN_ERR_UNSUPPORTED);
+    EXPECT(evict(true, 1 << 27), PASSED);
+  }
   printf("%s: %d failed expectations\n", failures ? "FAILED" : "ok", failures);
   return failures ? 1 : 0;
 }

@@ -521,8 +521,10 @@ dustin_status dustin_kv_commit(int32_t* seq_lens, const int32_t* accepted, const
  * beyond 6.  An infinity counts as the largest finite bf16 of its sign, a NaN as zero.
  *   k_new, v_new  bf16 [B, nq_max, Hkv, d] (d 64 or 128), strides in elements, as dustin_kv_append
  *   k, v          the caches; must address max_len + nq_max positions per sequence, with n_query max_len: then a sequence
- *                 needs room (pages) for its own N_b + T_b alone; rows past a cache's end are not written.  Sequences and heads
- *                 have places of their own (no stride of zero between them)
+ *                 needs room (pages) for its own N_b + T_b alone; rows past a cache's end are not written.  Sequences
+ *                 and heads have places of their own (no stride of zero between them).  The table's entries for the
+ *                 positions that are written name the sequence's pages: an id outside the pool counts as its nearest
+ *                 page, here as in every call
  *   bt            seq_lens (N_b), n_query (T_b, NULL = nq_max), max_len, nq_max
  * --------------------------------------------------------------------------------- */
 dustin_status dustin_kv4_append(const void* k_new, int64_t k_sb, int64_t k_st, int64_t k_sh, const void* v_new,

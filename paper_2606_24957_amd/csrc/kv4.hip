@@ -23,7 +23,7 @@ __global__ __launch_bounds__(kKv4Threads) void kv4_append_kernel(Kv4RowsArgs a, 
   if (t >= (uint32_t)T) return;
   const int64_t pos = (int64_t)N + t;
   const Kv4View& c = is_v ? a.v : a.k;
-  if (pos >= c.capacity) return;  // no room (or no page) for this position: nothing is written
+  if (pos >= c.capacity) return;  // past the cache, or the page table: nothing is written
   const uint16_t* src = (is_v ? a.v_in : a.k_in) + b * (is_v ? a.v_sb : a.k_sb) + t * (is_v ? a.v_st : a.k_st) +
                         h * (is_v ? a.v_sh : a.k_sh);
   const u32x4 x = load16(src + 8 * chunk);

@@ -29,7 +29,7 @@ struct Kv4View {
   int32_t page_shift, max_pages, num_pages;
   int64_t capacity;
 
-  // pos in [0, capacity)
+  // pos in [0, capacity); a page id outside the pool counts as its nearest end, for reads and for writes
   __device__ __forceinline__ int page_of(int b, int pos) const {
     return clampi(page_table[(int64_t)b * max_pages + (pos >> page_shift)], 0, num_pages - 1);
   }

@@ -6,9 +6,10 @@
 // largest.  It is described by the rank of its last token.  Three kernels:
 //   chunks  every workgroup takes a piece of a row: its largest logit, the sum of its weights against that, and where
 //           a filter needs it a histogram of counts and sums over eighths of octaves of the weight
-//   rows    these joined, the eighth in which the kept set ends; the tokens that have to be ranked are listed: all that may be kept where those are few (each is then
-//           compared with each), otherwise those of the last eighth (ranked by histograms of ever finer ranges); where
-//           even these are many, one workgroup reads the row as often as it takes
+//   rows    these joined, the eighth in which the kept set ends; the tokens that have to be ranked are listed: all that
+//           may be kept where those are few (kSampleFew), otherwise those of the last eighth.  A short list (kPairs) is
+//           ranked by comparing each token with each, a longer one by histograms of ever finer ranges; where the eighth
+//           holds more than a list, one workgroup reads the row as often as it takes
 //   rest    (verification) what is left of the target's distribution after the first rejected draft, and the draw
 // Weights are computed in 64-bit floating point and summed as integers, so results do not depend on the order of
 // work; see sample.hpp.
@@ -136,7 +137,7 @@ __device__ __forceinline__ double weight(const Exp2& exp2, float x, float top, d
   const double w = exp2(d);
   return w < 0x1p-45 ? 0.0 : w;
 }
-// ... as a multiple of 2^-44 (the mantissa bits of it + 2^52).  What lies below 2^-45.5 is rounded to zero.
+// ... as a multiple of 2^-44 (the mantissa bits of it + 2^52).  What lies below 2^-45 is rounded to zero.
 __device__ __forceinline__ double exponent_of(float x, float top, double scale) {
   double d = ((double)x - (double)top) * scale;
   if (top == INFINITY) d = x == INFINITY ? 0.0 : -46.0;
@@ -886,7 +887,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
       for (int j = tid; j < m; j += kRowThreads) w += sm_w[j];
       z = block_sum<kRowWaves>(w, sm_red);
     }
-    // all tokens whose weight is no less than 2^-45.5 of the largest
+    // all tokens that have a weight, and some without, which find_token leaves out
     const uint64_t end = lists ? plan.hi : whole_key(bin_key(top, s.scale, kSampleBins - 1));
 #pragma unroll 1
     for (int by_sum = 0; by_sum < 2; ++by_sum) {  // the last of the top_k, then the last that top_p keeps

@@ -12,10 +12,10 @@ constexpr int kSampleMaxVocab = 1 << kSampleIdxBits;
 
 // A token's weight, 2^((x - top) log2(e) / T) of the row's largest logit, is summed as a multiple of 2^-44: sums of
 // integers do not depend on their order, 2^18 tokens stay below 2^62, and a weight is off by at most 2^-45.  Weights
-// below 2^-45 count as zero.
+// below 2^-45, half a unit, count as zero.
 constexpr int kSampleFrac = 44;
-constexpr int kSampleBins = 368;     // eighths of octaves from the largest weight down to 2^-45.5, and a few
-constexpr int kSampleFew = 1024;     // tokens ranked by comparing each with each
+constexpr int kSampleBins = 368;     // eighths of octaves from the largest weight down to 2^-46
+constexpr int kSampleFew = 1024;     // tokens of a list that holds all that may be kept
 constexpr int kSampleList = 4096;    // tokens of a list
 constexpr int kSampleMaxWindow = 64; // tokens of a verification window
 constexpr int kSamplePieces = 1024;  // 16-byte pieces of a chunk of a row (with 512, 128 rows took 90 us for 72, one 24)

@@ -580,14 +580,15 @@ dustin_status dustin_dense_verify_attn_kv4(const void* q, int64_t q_sb, int64_t 
  *   k, v, k_out, v_out  caches of 64 or 128 channels.  k_out and v_out are other caches (other pages), or the same:
  *       equal data, strides and page tables mark the call as in place.  Caches that overlap in another way are not
  *       supported, nor is one of K and V in place alone (DUSTIN_ERR_INVALID_ARG).  k_out and v_out address at least
- *       k_max positions, which to other caches come to less than 32 GB a sequence.  v and v_out may be NULL (a cache of keys alone, as the scores read); one cache must not be
- *       given as both k and v, and a page that two sequences share must not be written (a stride of zero between
- *       sequences or heads of k_out or v_out: DUSTIN_ERR_INVALID_ARG).
+ *       k_max positions; to other caches these come to less than 32 GB a sequence (else DUSTIN_ERR_UNSUPPORTED).  v and
+ *       v_out may be NULL (a cache of keys alone, as the scores read); one cache must not be given as both k and v, and
+ *       a page that two sequences share must not be written (a stride of zero between sequences or heads of k_out or
+ *       v_out: DUSTIN_ERR_INVALID_ARG).
  *   idx, count  int32 [B, groups, >= k_max] (strides idx_sb, idx_sg) and [B * groups]; ascending positions (in place,
  *       others give rows of unspecified content); a position outside
  *       the cache counts as its nearest end; groups 1 or the KV head count
- *   w, w_out    fp32 [B, groups, >= w_len], [B, groups, >= k_max] (strides in elements) or both NULL; w_out may be w, with
- *               w's strides
+ *   w, w_out    fp32 [B, groups, >= w_len], [B, groups, >= k_max] (strides in elements) or both NULL; w_out may be w,
+ *               with w's strides
  *   new_lens    int32 [B] or NULL; may be the batch's seq_lens, which this call does not read
  * A step's layers share idx: pass w and new_lens with one of them.  Without any cache (k, v, k_out and v_out NULL) the
  * weights alone are moved, for any number of groups: other arrays over the same positions, such as a history.

@@ -115,8 +115,9 @@ class VerifyStep:
                 ops.append((plan_kv4_append if isinstance(L.k, KV4) else plan_kv_append)(
                     k_new, v_new, L.k, L.v, self.seq, n_query=self.nq, page_table=L.page_table, max_len=N,
                     stream=stream))
+            bound = dict(max_len=N) if isinstance(L.k, KV4) else {}  # (the lengths that its append takes)
             ops.append(_plan_sparse(L)(L.q, L.k, L.v, self.idx, self.cnt, self.seq, n_query=self.nq,
-                                       page_table=L.page_table, out=o, stream=stream))
+                                       page_table=L.page_table, out=o, stream=stream, **bound))
         return ops
 
     def run(self):

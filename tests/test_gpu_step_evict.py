@@ -180,3 +180,23 @@ def test_sequences_of_one_cache_are_not_cut_in_place():
         D.kv_evict(k.expand(3, 64, 2, 128), None, idx, cnt)
     D.kv_evict(k.expand(3, 64, 2, 128), None, idx, cnt, k_out=torch.empty((3, 8, 2, 128), dtype=torch.bfloat16, device=DEV))
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("preset", ["qwen7b", "ragged"])
+def test_a_step_over_4_bits_takes_one_length_in_all_its_calls(preset):
+    """Lengths past the planned ones (the caller's to avoid) are clamped alike by append and attention: the window that
+    the one writes is the window that the other reads."""
+    s = W.config(preset)
+    s = s.replace(B=2, seq_lens=(700, 300), n_query=(5, 3), budget=(128, 100), m=(54, 40), planted=(20, 20), layers=1)
+    layer = W.make_layer(s, 0, DEV)
+    est = W.make_estimation(s, layer, DEV)
+    four = S.layer4(s, layer)
+    st = S.VerifyStep(s, [four], est, DEV, windows=[S.window_kv(s, layer)], score_k=layer.k)
+    st.run()
+    torch.cuda.synchronize()
+    want = st.outs[0].clone()
+    st.seq[0] += 2
+    st.run()
+    torch.cuda.synchronize()
+    for b, t in enumerate(s.n_query):
+        assert torch.equal(st.outs[0][b, :t].view(torch.int16), want[b, :t].view(torch.int16))

@@ -17,10 +17,11 @@
 // decoding, the value tile's way through LDS and the barriers of a round are in the way (with 40 rows: vector unit 44 %,
 // matrix unit 27 %, LDS 40 % busy over a call).  Up to 48 query rows the registers and LDS are cut down so that two
 // workgroups fit a CU, and where there is much to do (kAttn4Much) both are used: whole calls over 8 sequences of 32768
-// tokens and 8 KV heads take 70 us (8 rows, 4.1 TB/s), 91 (32) and 108 (40), with one workgroup to a CU, that has two
-// value tiles and more rounds in flight, 84, 107 and 119; the same over 4096 selected ones (2112 granules) 24, 27 and 31
-// either way with one workgroup to a CU, 24, 29 and 32 with two.  With more rows there is no room for a second:
-// 72 rows 133 us, 88 155, 128 221; 16 sequences of 4000 to 65536 tokens, 72 rows, pages of 16: 291 (2.1 TB/s).
+// tokens and 8 KV heads take 73 us (8 rows, 3.9 TB/s), 89 (32) and 102 (40); with one workgroup to a CU, that has two
+// value tiles and more rounds in flight, these were 84, 107 and 119.  The same over 4096 selected ones (2112 granules)
+// take 22, 25 and 29; there one workgroup to a CU was no slower (24, 27 and 31 for 24, 29 and 32 with two).  With more
+// rows there is no room for a second: 72 rows 133 us, 88 150, 128 223; 16 sequences of 4000 to 65536 tokens, 72 rows,
+// pages of 16: 293 (2.1 TB/s).
 // Other forms: one value tile and two barriers a round with 72 rows 133, 88 161; the queries read from LDS as well
 // 148 and 176; every wave with tokens and an accumulator of its own, joined at the end of a part, 46 where this form at
 // its first took 36.
